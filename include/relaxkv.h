@@ -22,6 +22,13 @@
  * completion: the query tokens' attention over the repaired cache, whose row
  * log-sum-exp feeds the one-pass scoring mode (relaxkv_query_attn; App. C.4).
  *
+ * Around that path, for a program that serves a repaired cache to many requests at
+ * once: the norm and rotation that turn projections into the rows every call takes
+ * (relaxkv_fresh_rows, relaxkv_batch_rows), the row maps of a step
+ * (relaxkv_batch_plan), the attention of all requests over the shared context
+ * (relaxkv_shared_attn) or over the context blocks that a score selects for each row
+ * (relaxkv_block_means, relaxkv_block_select, relaxkv_block_attn).
+ *
  * Conventions shared by every call
  * --------------------------------
  * - Device pointers are HIP device memory of the current device; host
@@ -474,6 +481,207 @@ relaxkv_status relaxkv_query_attn_noalloc(const relaxkv_problem* p, int32_t laye
  */
 relaxkv_status relaxkv_counts_to_host(const relaxkv_sets* s, int32_t* host_counts,
                                       int64_t* host_edges, void* stream);
+
+/* ------------------------------------------------------------------------------
+ * Batched serving of one context cache.
+ *
+ * A batch is n_seq requests that share the problem's T_c context positions.  Each owns a
+ * suffix of at most max_suffix tokens after the context (its question, what it has
+ * generated), whose keys and values lie in suffix caches of the caller.  One step brings
+ * new_b >= 0 new tokens for request b (one while it decodes, several while its question is
+ * read, none while it rests) behind the past_b it has; the step's rows are the new tokens of
+ * request 0, then those of request 1, and so on.  A step runs
+ *   relaxkv_batch_plan, then per layer relaxkv_batch_rows (rotated queries; the new keys and
+ *   values into the suffix caches) and relaxkv_shared_attn, or relaxkv_block_select and
+ *   relaxkv_block_attn.
+ */
+#define RELAXKV_MAX_SEQS 65536
+#define RELAXKV_MAX_BATCH_ROWS 65536
+#define RELAXKV_MAX_BATCH_ROW_HEADS (1 << 22)      /* n_rows * H */
+#define RELAXKV_MAX_SELECTED_BLOCKS 2048
+
+/* Bit of a batch's error word counts[3]. */
+#define RELAXKV_BATCH_ERR_LENGTHS 1  /* a length below 0, past_b + new_b > max_suffix, or more
+                                        than n_rows new tokens: the plan is then empty */
+
+/*
+ * The maps of a step, carved by relaxkv_batch_bind out of one caller-owned device buffer
+ * and written by relaxkv_batch_plan.
+ *   n_seq, n_rows, max_suffix  requests; rows that the caller's row buffers hold (>= 0; a
+ *            step may have fewer); tokens of a request's suffix.
+ *   row_off  [n_seq+1]  request b's rows are row_off[b] .. row_off[b+1]-1.
+ *   row_seq  [n_rows]   request of each row, -1 behind the step's last row.
+ *   row_pos  [n_rows]   position T_c + past_b + i of each row, -1 behind the last.
+ *   tiles    [tile_cap][8]  the attention's row tiles (internal).
+ *   counts   [4]        rows of the step, row tiles, 0, error word.
+ * T_c, H, H_kv, d and dtype are those of the problem the batch was bound for; every call
+ * refuses a batch of another shape.
+ */
+typedef struct relaxkv_batch {
+    int32_t n_seq, n_rows, max_suffix, tile_cap;
+    int32_t T_c, H, H_kv, d, dtype;
+    int32_t* row_off;
+    int32_t* row_seq;
+    int32_t* row_pos;
+    int32_t* tiles;
+    int32_t* counts;
+} relaxkv_batch;
+
+/* The suffix caches of one layer: token i of request b and KV head g is the d contiguous
+ * elements from b * stride_seq + g * stride_head + i * stride_token of k and of v.  0
+ * selects the dense strides of [n_seq][H_kv][max_suffix][d].  The rules of the context
+ * cache's strides hold (rows that do not overlap, 16-byte aligned); a token stride is below
+ * 2^24 elements.  Tokens past a request's length are neither read nor written. */
+typedef struct relaxkv_suffix {
+    void* k;
+    void* v;
+    int64_t stride_seq, stride_head, stride_token;
+} relaxkv_suffix;
+
+/* Norm and rotation of a model.
+ *   inv_freq   device [rot/2] float32: the angle of pair i at position P is P * inv_freq[i]
+ *              (may be NULL when rot is 0).
+ *   q_weight, k_weight  device [d] in dtype: weights of the RMS norm over each head's d
+ *              values; NULL for no norm.
+ *   eps        added to the mean square (finite, >= 0).
+ *   rot        rotated values of a head: a multiple of 16, 0 <= rot <= d.
+ *   interleaved  0: pairs (i, i + rot/2); 1: pairs (2i, 2i + 1). */
+typedef struct relaxkv_rope {
+    const float* inv_freq;
+    const void* q_weight;
+    const void* k_weight;
+    float eps;
+    int32_t rot, interleaved;
+} relaxkv_rope;
+
+/* Rows of a projection: row i's heads, [H][d] for q and [H_kv][d] for k and v, start at
+ * element i * stride (0: dense), so the three may be slices of one fused output.  A NULL
+ * pointer leaves that kind out. */
+typedef struct relaxkv_rows {
+    const void* q;
+    const void* k;
+    const void* v;
+    int64_t q_stride, k_stride, v_stride;
+    int32_t n_rows;
+} relaxkv_rows;
+
+/* Host only.  Device bytes of a batch's maps (0 for bad arguments: n_seq in [1,
+ * RELAXKV_MAX_SEQS], n_rows in [0, RELAXKV_MAX_BATCH_ROWS] with n_rows * H at most
+ * RELAXKV_MAX_BATCH_ROW_HEADS, max_suffix in [1, RELAXKV_MAX_TC]). */
+size_t relaxkv_batch_bytes(const relaxkv_problem* p, int32_t n_seq, int32_t n_rows,
+                           int32_t max_suffix);
+
+/* Host only.  Fills *out with the sizes and pointers carved out of dev_buf (256-byte
+ * aligned).  RELAXKV_ENOSPACE when bytes < relaxkv_batch_bytes(...). */
+relaxkv_status relaxkv_batch_bind(const relaxkv_problem* p, int32_t n_seq, int32_t n_rows,
+                                  int32_t max_suffix, void* dev_buf, size_t bytes,
+                                  relaxkv_batch* out);
+
+/*
+ * Row maps of a step.  past_len, new_len: device [n_seq] int32.  Writes every array of b.  A bad
+ * length (RELAXKV_BATCH_ERR_LENGTHS) sets the error word and leaves a step without rows, for
+ * which the other calls do nothing.
+ */
+relaxkv_status relaxkv_batch_plan(const relaxkv_problem* p, const relaxkv_batch* b,
+                                  const int32_t* past_len, const int32_t* new_len, void* stream);
+
+/* Synchronising.  Copies b->counts to host_counts[4] after all work queued on `stream`.
+ * RELAXKV_EINVAL while the error word is set (the counts are still copied). */
+relaxkv_status relaxkv_batch_to_host(const relaxkv_batch* b, int32_t* host_counts, void* stream);
+
+/*
+ * Norm (where the weights are given) and rotation of the rows of a projection at explicit
+ * positions, values copied: dense rows as the fresh rows of relaxkv_sparse_attn (positions
+ * s->R_idx + R_off[l]), the queries and k_q/v_q of relaxkv_query_attn (positions T_c ..), or
+ * the rows of a cache that moves (positions may be negative).  Per head
+ *   y_i = x_i / sqrt(mean_j x_j^2 + eps) * w_i,
+ *   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = position * inv_freq[pair],
+ * in float32 (the angle in 64 bits), rounded once.
+ *   positions  device [n_rows] int32.
+ *   q_out      device [n_rows][H][d], k_out and v_out [n_rows][H_kv][d] in dtype; NULL exactly
+ *              where the input is.  An output may be its own dense input; otherwise outputs
+ *              and inputs do not overlap.
+ */
+relaxkv_status relaxkv_fresh_rows(const relaxkv_problem* p, const relaxkv_rope* r,
+                                  const relaxkv_rows* in, const int32_t* positions, void* q_out,
+                                  void* k_out, void* v_out, void* stream);
+
+/*
+ * The same for the rows of a planned step, at their positions: queries to q_out
+ * [n_rows][H][d], keys and values to the suffix tokens row_pos - T_c of their requests.
+ * in->n_rows must be b->n_rows; rows behind the step's last are neither read nor written.
+ */
+relaxkv_status relaxkv_batch_rows(const relaxkv_problem* p, const relaxkv_rope* r,
+                                  const relaxkv_batch* b, const relaxkv_rows* in, void* q_out,
+                                  const relaxkv_suffix* suffix, void* stream);
+
+/* Host only.  Device scratch bytes of relaxkv_shared_attn (0 for float32, and for bad
+ * arguments). */
+size_t relaxkv_shared_attn_workspace_bytes(const relaxkv_problem* p, const relaxkv_batch* b);
+
+/*
+ * Attention of a planned step's rows at layer `layer` over the shared context and,
+ * causally, the own request's suffix:
+ *   O_{t,h} = sum_j softmax_j(sigma <q_{t,h}, K_j>) V_j,  j over the T_c context positions and
+ *   then the suffix tokens 0 .. row_pos[t] - T_c of request row_seq[t].
+ * The context's keys and values are read once for all requests.
+ *   k_cache, v_cache  device [L][H_kv][T_c][d] in dtype with the problem's strides.
+ *   q         device [n_rows][H][d] in dtype (rotated).
+ *   suffix    the layer's suffix caches, which already hold the step's new tokens.
+ *   out       device out [n_rows][H][d] in dtype; lse_out optional [n_rows][H] float32, the
+ *             natural-log normaliser.  Rows behind the step's last are left as they are.
+ *   ws        device scratch of ws_bytes >= relaxkv_shared_attn_workspace_bytes(p, b); two
+ *             calls that share it must be ordered.
+ * The same call gives the same bits on every run; the last bits depend on n_rows, n_seq,
+ * max_suffix and T_c, which choose the splits.
+ */
+relaxkv_status relaxkv_shared_attn(const relaxkv_problem* p, const relaxkv_batch* b, int32_t layer,
+                                   const void* k_cache, const void* v_cache, const void* q,
+                                   const relaxkv_suffix* suffix, void* out, float* lse_out,
+                                   void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Means of the cached keys over blocks of `block` positions (16, 32, 64 or 128; the last
+ * block may be shorter), summed in 64 bits and rounded once.
+ *   layer   a layer, or -1 for all of them.
+ *   means   device out [n][H_kv][ceil(T_c / block)][d] in dtype, n = 1 or L.
+ */
+relaxkv_status relaxkv_block_means(const relaxkv_problem* p, int32_t layer, const void* k_cache,
+                                   int32_t block, void* means, void* stream);
+
+/* Host only.  Device scratch bytes of relaxkv_block_select (0 for bad arguments). */
+size_t relaxkv_block_select_workspace_bytes(const relaxkv_problem* p, const relaxkv_batch* b,
+                                            int32_t block);
+
+/*
+ * Context blocks of each row of a planned step and KV head g: the n_sel blocks j with the
+ * largest s_j = <sum of the queries of g's heads, means_j>, summed in 64 bits and rounded to
+ * float32 once; equal ones to the lower block (-0 equals +0), a NaN below every number; in
+ * ascending order.
+ *   means   device [H_kv][ceil(T_c / block)][d] in dtype: one layer's block means.
+ *   q       device [n_rows][H][d] in dtype.
+ *   n_sel   1 .. min(ceil(T_c / block), RELAXKV_MAX_SELECTED_BLOCKS).
+ *   blocks  device out [n_rows][H_kv][n_sel] int32; rows behind the step's last are left.
+ */
+relaxkv_status relaxkv_block_select(const relaxkv_problem* p, const relaxkv_batch* b, int32_t block,
+                                    const void* means, const void* q, int32_t n_sel,
+                                    int32_t* blocks, void* ws, size_t ws_bytes, void* stream);
+
+/* Host only.  Device scratch bytes of relaxkv_block_attn (0 for float32 and bad arguments). */
+size_t relaxkv_block_attn_workspace_bytes(const relaxkv_problem* p, const relaxkv_batch* b,
+                                          int32_t block, int32_t n_sel);
+
+/*
+ * relaxkv_shared_attn with the context replaced, per row and KV head, by the positions of
+ * listed blocks.
+ *   blocks  device [n_rows][H_kv][n_sel] int32, in any order: an entry outside
+ *           [0, ceil(T_c / block)) is no block, one that is listed twice counts twice.
+ */
+relaxkv_status relaxkv_block_attn(const relaxkv_problem* p, const relaxkv_batch* b, int32_t layer,
+                                  const void* k_cache, const void* v_cache, int32_t block,
+                                  const int32_t* blocks, int32_t n_sel, const void* q,
+                                  const relaxkv_suffix* suffix, void* out, float* lse_out,
+                                  void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

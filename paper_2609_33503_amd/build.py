@@ -50,7 +50,8 @@ def _hipcc():
 # the 32K workload than the default; the same instructions, reordered).
 PER_FILE = {"attn.hip": ["-fno-honor-nans", "-mllvm", "-amdgpu-sched-strategy=max-ilp"],
             "score.hip": ["-fno-honor-nans"],
-            "query_attn.hip": ["-fno-honor-nans"]}
+            "query_attn.hip": ["-fno-honor-nans"],
+            "batch_attn.hip": ["-fno-honor-nans"]}
 
 
 def _sources(root):

@@ -1,0 +1,314 @@
+// Block means of the cached keys, and the context blocks that a score by those means
+// selects for each row and KV head.
+//
+//   m_j = (1 / n_j) sum_{i in block j} k_i                          (64-bit sums, rounded once)
+//   s_j = float32( sum_c (sum_{h in group} q_{h,c}) m_{j,c} )       (64-bit sums)
+//   the n_sel largest s_j, equal ones to the lower block, in ascending block order.
+//
+// A selection is only as reproducible as its scores: float32 sums of another order differ in
+// the last bits and swap blocks near the border.  Products of two bf16 (or float32) values
+// are exact in 64 bits and their sums there are off by 2^-53, so the score that is
+// rounded to float32 is, but for one in about 2^28, the same whatever the order of its sum.
+// The 64-bit rate of the chip (half its float32 rate) makes that cheap: 2 nb d operations
+// per row and KV head, against 4 G d per key of the attention that follows.
+//
+// block_means is memory bound (reads every key once); the scores' products are few, and the
+// top-k of up to 4096 blocks runs in the registers of one wave per row, by binary search over
+// the key's bits with no barrier.
+
+#include <algorithm>
+
+#include "batch.h"
+#include "dev_common.h"
+
+namespace relaxkv {
+namespace {
+
+template <typename T> __device__ __forceinline__ void load8(const T* p, float* f);
+template <> __device__ __forceinline__ void load8<uint16_t>(const uint16_t* p, float* f) {
+    const u32x4 r = *(const u32x4*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(r[i] << 16);
+        f[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+    }
+}
+template <> __device__ __forceinline__ void load8<float>(const float* p, float* f) {
+    const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[i] = a[i];
+        f[4 + i] = b[i];
+    }
+}
+
+// One wave per block: D/8 lanes take a key's row, 512/D keys at a time.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void block_means(const T* __restrict__ k, KvStrides ks,
+                                                   int layer0, int n_heads, int Hkv, int nb, int T_c,
+                                                   int block, T* __restrict__ means) {
+    constexpr int LPK = D / 8, KPW = 64 / LPK;
+    const int lane = threadIdx.x & 63, c = lane % LPK, r = lane / LPK;
+    const long units = (long)n_heads * nb;                        // (layer, head, block)
+    for (long unit = blockIdx.x * 4l + (threadIdx.x >> 6); unit < units; unit += gridDim.x * 4l) {
+        const int lg = (int)(unit / nb), j = (int)(unit - (long)lg * nb);
+        const int l = lg / Hkv, g = lg - l * Hkv;
+        const int i0 = j * block, n = min(block, T_c - i0);
+        const T* src = k + (layer0 + l) * ks.layer + g * ks.head + (int64_t)i0 * ks.token + c * 8;
+        double acc[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = 0.0;
+#pragma unroll 4
+        for (int i = r; i < n; i += KPW) {
+            float f[8];
+            load8<T>(src + i * ks.token, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] += (double)f[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int o = LPK; o < 64; o <<= 1) acc[e] += __shfl_xor(acc[e], o, 64);
+        if (r == 0) {
+            T* dst = means + unit * D + c * 8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const double m = acc[e] / n;
+                if constexpr (sizeof(T) == 4) {
+                    dst[e] = (float)m;
+                } else {
+                    // Rounded once: through float32 to odd (a truncated float32 whose last bit
+                    // remembers what was cut off), from which the rounding to bf16 is that of m.
+                    float x = (float)m;
+                    uint32_t u = __float_as_uint(x);
+                    if ((double)x != m && x == x) {
+                        if (fabs((double)x) > fabs(m)) --u;
+                        u |= 1;
+                    }
+                    dst[e] = (u & 0x7fffffffu) > 0x7f800000u ? (uint16_t)((u >> 16) | 0x40)
+                                                             : f32_to_bf16_bits(__uint_as_float(u));
+                }
+            }
+        }
+    }
+}
+
+constexpr int kScoreTokens = 8;        // rows a workgroup scores against its 64 blocks
+
+// Four lanes per block, each a quarter of the head dimension in 8-element chunks.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void block_scores(const T* __restrict__ q,
+                                                    const T* __restrict__ means,
+                                                    const int32_t* __restrict__ counts, int n_rows,
+                                                    int H, int Hkv, int G, int nb,
+                                                    float* __restrict__ scores) {
+    constexpr int NT = kScoreTokens;
+    __shared__ __attribute__((aligned(16))) double qs[NT][D];
+    const int tid = threadIdx.x, g = blockIdx.y, t0 = blockIdx.z * NT;
+    const int rows = min(counts[0], n_rows);
+    if (t0 >= rows) return;
+    const int part = tid & 3, b = blockIdx.x * 64 + (tid >> 2);
+    const T* m = means + ((size_t)g * nb + min(b, nb - 1)) * D;
+    float mf[8];
+    load8<T>(m + part * 8, mf);
+    for (int x = tid; x < NT * D; x += 256) {
+        const int t = x / D, c = x - t * D;
+        double s = 0.0;
+        if (t0 + t < rows) {
+            const T* p = q + ((size_t)(t0 + t) * H + g * G) * D + c;
+            for (int h = 0; h < G; ++h) {
+                if constexpr (sizeof(T) == 2) s += (double)bf16_bits_to_f32(p[h * D]);
+                else s += (double)p[h * D];
+            }
+        }
+        qs[t][c] = s;
+    }
+    __syncthreads();
+    double acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = 0.0;
+#pragma unroll 1
+    for (int i = 0; i < D / 32; ++i) {                     // (not unrolled, for the registers)
+        const int c0 = (part + 4 * i) * 8;
+        float nf[8];
+        if (i + 1 < D / 32) load8<T>(m + c0 + 32, nf);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const double x = (double)mf[e];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[t] = fma(qs[t][c0 + e], x, acc[t]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mf[e] = nf[e];
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        acc[t] += __shfl_xor(acc[t], 1, 64);
+        acc[t] += __shfl_xor(acc[t], 2, 64);
+        if (part == (t & 3) && b < nb && t0 + t < rows)
+            scores[((size_t)(t0 + t) * Hkv + g) * nb + b] = (float)acc[t];
+    }
+}
+
+// Ascending with the score; -0 as +0; NaN below every number.
+__device__ __forceinline__ uint32_t score_key(float f) {
+    uint32_t u = __float_as_uint(f);
+    if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;
+    if (u == 0x80000000u) u = 0u;
+    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// One wave per (row, KV head), block e * 64 + lane in register e.  The k-th largest key is
+// the largest t with at least k keys >= t.  Blocks past nb hold key 0; a NaN's key 0
+// lies at a lower block, and k <= nb, so none of them is ever taken.
+template <int E>
+__global__ __launch_bounds__(256) void block_topk_wave(const float* __restrict__ scores, int nb,
+                                                       int k, const int32_t* __restrict__ counts,
+                                                       int n_rows, int Hkv,
+                                                       int32_t* __restrict__ out) {
+    const long unit = blockIdx.x * 4l + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (unit >= (long)min(counts[0], n_rows) * Hkv) return;
+    const float* s = scores + unit * nb;
+    uint32_t key[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int i = e * 64 + lane;
+        key[e] = i < nb ? score_key(s[i]) : 0u;
+    }
+    uint32_t t = 0;
+#pragma unroll 1
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t cand = t | (1u << bit);
+        int n = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) n += __popcll(__ballot(key[e] >= cand));
+        if (n >= k) t = cand;
+    }
+    int above = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) above += __popcll(__ballot(key[e] > t));
+    const int need = k - above;                      // of the keys equal to t, the first ones
+    int gt0 = 0, eq0 = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const uint64_t mg = __ballot(key[e] > t), me = __ballot(key[e] == t);
+        const int gt = gt0 + lanes_below(mg), eq = eq0 + lanes_below(me);
+        if (key[e] > t || (key[e] == t && eq < need))
+            out[unit * k + gt + min(eq, need)] = e * 64 + lane;
+        gt0 += __popcll(mg);
+        eq0 += __popcll(me);
+    }
+}
+
+// Rows of any length: one workgroup per (row, KV head) reads its scores once per 8-bit
+// digit and once for the compaction.
+__global__ __launch_bounds__(256) void block_topk_long(const float* __restrict__ scores, int nb,
+                                                       int k, const int32_t* __restrict__ counts,
+                                                       int n_rows, int Hkv,
+                                                       int32_t* __restrict__ out) {
+    __shared__ int hist[256], scratch[4];
+    __shared__ int digit_sh, above_sh;
+    const long unit = blockIdx.x;
+    const int tid = threadIdx.x;
+    if (unit >= (long)min(counts[0], n_rows) * Hkv) return;
+    const float* s = scores + unit * nb;
+    uint32_t t = 0, mask = 0;
+    int need = k;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        hist[tid] = 0;
+        __syncthreads();
+        for (int i = tid; i < nb; i += 256) {
+            const uint32_t key = score_key(s[i]);
+            if ((key & mask) == t) atomicAdd(&hist[(key >> shift) & 255], 1);
+        }
+        __syncthreads();
+        int total;
+        const int h = hist[255 - tid];
+        const int before = block_exclusive_scan<256>(h, scratch, total);
+        if (before < need && before + h >= need) {
+            digit_sh = 255 - tid;
+            above_sh = before;
+        }
+        __syncthreads();
+        t |= (uint32_t)digit_sh << shift;
+        mask |= 255u << shift;
+        need -= above_sh;
+        __syncthreads();
+    }
+    int gt0 = 0, eq0 = 0;
+    for (int i0 = 0; i0 < nb; i0 += 256) {
+        const int i = i0 + tid;
+        const uint32_t key = i < nb ? score_key(s[i]) : 0u;
+        const bool g = i < nb && key > t, e = i < nb && key == t;
+        int total;
+        const int sc = block_exclusive_scan<256>((g ? 1 : 0) | (e ? 1 << 16 : 0), scratch, total);
+        const int gt = gt0 + (sc & 0xffff), eq = eq0 + (sc >> 16);
+        if (g || (e && eq < need)) out[unit * k + gt + min(eq, need)] = i;
+        gt0 += total & 0xffff;
+        eq0 += total >> 16;
+    }
+}
+
+template <typename T, int D>
+void launch_means(const relaxkv_problem& p, int layer0, int n_layers, const void* k, int block,
+                  void* means, hipStream_t st) {
+    const int nb = block_count(p, block), heads = n_layers * p.H_kv;
+    const long units = (long)heads * nb;
+    hipLaunchKernelGGL((block_means<T, D>), dim3((unsigned)std::min((units + 3) / 4, 1l << 22)), dim3(256), 0,
+                       st, (const T*)k, kv_strides(p), layer0, heads, p.H_kv, nb, p.T_c, block,
+                       (T*)means);
+}
+
+template <typename T, int D>
+void launch_scores(const relaxkv_problem& p, const relaxkv_batch& b, int block, const void* means,
+                   const void* q, float* scores, hipStream_t st) {
+    const int nb = block_count(p, block);
+    hipLaunchKernelGGL((block_scores<T, D>),
+                       dim3((nb + 63) / 64, p.H_kv, (b.n_rows + kScoreTokens - 1) / kScoreTokens),
+                       dim3(256), 0, st, (const T*)q, (const T*)means, b.counts, b.n_rows, p.H,
+                       p.H_kv, p.H / p.H_kv, nb, scores);
+}
+
+}  // namespace
+
+size_t block_select_bytes(const relaxkv_problem& p, const relaxkv_batch& b, int block) {
+    return ((size_t)b.n_rows * p.H_kv * block_count(p, block) * 4 + 255) / 256 * 256;
+}
+
+hipError_t launch_block_means(const relaxkv_problem& p, int layer0, int n_layers,
+                              const void* k_cache, int block, void* means, hipStream_t st) {
+    if (p.dtype == RELAXKV_DTYPE_BF16) {
+        if (p.d == 128) launch_means<uint16_t, 128>(p, layer0, n_layers, k_cache, block, means, st);
+        else launch_means<uint16_t, 64>(p, layer0, n_layers, k_cache, block, means, st);
+    } else {
+        if (p.d == 128) launch_means<float, 128>(p, layer0, n_layers, k_cache, block, means, st);
+        else launch_means<float, 64>(p, layer0, n_layers, k_cache, block, means, st);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_block_select(const relaxkv_problem& p, const relaxkv_batch& b, int block,
+                               const void* means, const void* q, int n_sel, int32_t* blocks,
+                               float* scores, hipStream_t st) {
+    if (p.dtype == RELAXKV_DTYPE_BF16) {
+        if (p.d == 128) launch_scores<uint16_t, 128>(p, b, block, means, q, scores, st);
+        else launch_scores<uint16_t, 64>(p, b, block, means, q, scores, st);
+    } else {
+        if (p.d == 128) launch_scores<float, 128>(p, b, block, means, q, scores, st);
+        else launch_scores<float, 64>(p, b, block, means, q, scores, st);
+    }
+    const int nb = block_count(p, block);
+    const long units = (long)b.n_rows * p.H_kv;
+    auto go = [&](auto kernel, long per_wg) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((units + per_wg - 1) / per_wg)), dim3(256), 0, st,
+                           scores, nb, n_sel, b.counts, b.n_rows, p.H_kv, blocks);
+    };
+    if (nb <= 4 * 64) go(block_topk_wave<4>, 4);
+    else if (nb <= 16 * 64) go(block_topk_wave<16>, 4);
+    else if (nb <= 64 * 64) go(block_topk_wave<64>, 4);
+    else go(block_topk_long, 1);
+    return hipGetLastError();
+}
+
+}  // namespace relaxkv

@@ -23,6 +23,18 @@ inline KvStrides kv_strides(const relaxkv_problem& p) {
     return s;
 }
 
+// One dimension of a strided array outside its contiguous head dimension.
+struct StrideDim {
+    int64_t stride, n;
+};
+
+// RELAXKV_OK when three dimensions over rows of d contiguous elements do not overlap: taken
+// from the smallest, each stride of a dimension with more than one entry steps past the
+// whole extent of the dimensions inside it (else RELAXKV_EINVAL); and when every such stride
+// is a multiple of `align` elements and the extent is below 2^48 elements, which no device
+// holds and whose offsets fit in 64 bits (else RELAXKV_EUNSUPPORTED).  Sorts dims.
+relaxkv_status strides_nest(StrideDim (&dims)[3], int64_t d, int64_t align);
+
 // Scratch layout of relaxkv_score (offsets in bytes from the workspace base).
 struct ScoreWorkspace {
     size_t part_off;    // float [L][n_part][T_c]   per-KV-head pooled partial sums

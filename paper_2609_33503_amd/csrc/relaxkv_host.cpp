@@ -70,30 +70,16 @@ bool sets_match(const relaxkv_problem* p, const relaxkv_sets* s) {
 relaxkv_status strides_status(const relaxkv_problem* p) {
     if (p->kv_stride_layer < 0 || p->kv_stride_head < 0 || p->kv_stride_token < 0)
         return RELAXKV_EINVAL;
-    constexpr int64_t kMaxExtent = (int64_t)1 << 48;
     // The dense defaults (as kv_strides forms them), with overflow checks.
     int64_t sT = p->kv_stride_token ? p->kv_stride_token : p->d, sH, sL;
     if (p->kv_stride_head) sH = p->kv_stride_head;
     else if (__builtin_mul_overflow((int64_t)p->T_c, sT, &sH)) return RELAXKV_EUNSUPPORTED;
     if (p->kv_stride_layer) sL = p->kv_stride_layer;
     else if (__builtin_mul_overflow((int64_t)p->H_kv, sH, &sL)) return RELAXKV_EUNSUPPORTED;
-    struct Dim { int64_t stride, n; } dims[3] = {{sT, p->T_c}, {sH, p->H_kv}, {sL, p->L}};
-    for (int i = 1; i < 3; ++i)                          // ascending strides (insertion sort)
-        for (int j = i; j > 0 && dims[j].stride < dims[j - 1].stride; --j) {
-            const Dim t = dims[j];
-            dims[j] = dims[j - 1];
-            dims[j - 1] = t;
-        }
+    StrideDim dims[3] = {{sT, p->T_c}, {sH, p->H_kv}, {sL, p->L}};
     const int64_t align = p->dtype == RELAXKV_DTYPE_BF16 ? 8 : 4;   // elements per 16 bytes
-    int64_t extent = p->d;                               // elements spanned by the inner dimensions
-    for (const Dim& dm : dims) {
-        if (dm.n <= 1) continue;
-        if (dm.stride < extent) return RELAXKV_EINVAL;
-        if (dm.stride % align) return RELAXKV_EUNSUPPORTED;
-        // extent += (n - 1) * stride, kept below 2^48
-        if (dm.stride > (kMaxExtent - extent) / (dm.n - 1)) return RELAXKV_EUNSUPPORTED;
-        extent += (dm.n - 1) * dm.stride;
-    }
+    const relaxkv_status nest = strides_nest(dims, p->d, align);
+    if (nest != RELAXKV_OK) return nest;
     if ((uintptr_t)p->q % 16 || (uintptr_t)p->k_cache % 16 || (uintptr_t)p->v_cache % 16)
         return RELAXKV_EUNSUPPORTED;
     // (the bf16 attention forms the offset with a 24-bit multiply)
@@ -107,6 +93,30 @@ relaxkv_status strides_status(const relaxkv_problem* p) {
 relaxkv_status from_hip(hipError_t e) { return e == hipSuccess ? RELAXKV_OK : RELAXKV_EDEVICE; }
 
 }  // namespace
+
+namespace relaxkv {
+
+relaxkv_status strides_nest(StrideDim (&dims)[3], int64_t d, int64_t align) {
+    constexpr int64_t kMaxExtent = (int64_t)1 << 48;
+    for (int i = 1; i < 3; ++i)                          // ascending strides (insertion sort)
+        for (int j = i; j > 0 && dims[j].stride < dims[j - 1].stride; --j) {
+            const StrideDim t = dims[j];
+            dims[j] = dims[j - 1];
+            dims[j - 1] = t;
+        }
+    int64_t extent = d;                                  // elements spanned by the inner dimensions
+    for (const StrideDim& dm : dims) {
+        if (dm.n <= 1) continue;
+        if (dm.stride < extent) return RELAXKV_EINVAL;
+        if (dm.stride % align) return RELAXKV_EUNSUPPORTED;
+        // extent += (n - 1) * stride, kept below 2^48
+        if (dm.stride > (kMaxExtent - extent) / (dm.n - 1)) return RELAXKV_EUNSUPPORTED;
+        extent += (dm.n - 1) * dm.stride;
+    }
+    return RELAXKV_OK;
+}
+
+}  // namespace relaxkv
 
 extern "C" {
 

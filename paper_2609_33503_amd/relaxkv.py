@@ -22,6 +22,8 @@ ERR_NAN_SCORE, ERR_BAD_TARGETS, ERR_ROWS = 1, 2, 4      # bits of the device err
 DTYPE_F32, DTYPE_BF16 = 0, 1
 CONTEXT_UNION, CONTEXT_FULL = 0, 1
 CONTEXT_SETS_UNION, CONTEXT_SETS_GLOBAL, CONTEXT_SETS_LAYERWISE = 0, 1, 2
+BATCH_ERR_LENGTHS = 1                                   # bit of a batch's error word
+MAX_SELECTED_BLOCKS = 2048
 
 EXPORTS = ("relaxkv_status_string", "relaxkv_anchor_count", "relaxkv_validate",
            "relaxkv_score_workspace_bytes", "relaxkv_sets_bytes", "relaxkv_sets_bind",
@@ -29,7 +31,12 @@ EXPORTS = ("relaxkv_status_string", "relaxkv_anchor_count", "relaxkv_validate",
            "relaxkv_select_global",
            "relaxkv_build_sets_global", "relaxkv_sparse_attn", "relaxkv_update_cache",
            "relaxkv_query_attn_workspace_bytes", "relaxkv_query_attn",
-           "relaxkv_query_attn_noalloc", "relaxkv_counts_to_host")
+           "relaxkv_query_attn_noalloc", "relaxkv_counts_to_host",
+           "relaxkv_batch_bytes", "relaxkv_batch_bind", "relaxkv_batch_plan",
+           "relaxkv_batch_to_host", "relaxkv_fresh_rows", "relaxkv_batch_rows",
+           "relaxkv_shared_attn_workspace_bytes", "relaxkv_shared_attn", "relaxkv_block_means",
+           "relaxkv_block_select_workspace_bytes", "relaxkv_block_select",
+           "relaxkv_block_attn_workspace_bytes", "relaxkv_block_attn")
 QUERY_ATTN_NOALLOC_MAX_BYTES = 32 << 20
 
 
@@ -55,6 +62,28 @@ class Sets(Structure):
                 ("src", c_void_p), ("rank", c_void_p), ("counts", c_void_p),
                 ("edges", c_void_p), ("ctx", c_void_p), ("g", c_void_p), ("tiles", c_void_p),
                 ("global_targets", c_int32), ("context_sets", c_int32)]
+
+
+class CBatch(Structure):
+    _fields_ = [("n_seq", c_int32), ("n_rows", c_int32), ("max_suffix", c_int32),
+                ("tile_cap", c_int32), ("T_c", c_int32), ("H", c_int32), ("H_kv", c_int32),
+                ("d", c_int32), ("dtype", c_int32), ("row_off", c_void_p), ("row_seq", c_void_p),
+                ("row_pos", c_void_p), ("tiles", c_void_p), ("counts", c_void_p)]
+
+
+class CSuffix(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("stride_seq", c_int64),
+                ("stride_head", c_int64), ("stride_token", c_int64)]
+
+
+class CRope(Structure):
+    _fields_ = [("inv_freq", c_void_p), ("q_weight", c_void_p), ("k_weight", c_void_p),
+                ("eps", c_float), ("rot", c_int32), ("interleaved", c_int32)]
+
+
+class CRows(Structure):
+    _fields_ = [("q", c_void_p), ("k", c_void_p), ("v", c_void_p), ("q_stride", c_int64),
+                ("k_stride", c_int64), ("v_stride", c_int64), ("n_rows", c_int32)]
 
 
 _lib = None
@@ -119,6 +148,44 @@ def load(path=None):
     lib.relaxkv_counts_to_host.restype = c_int32
     lib.relaxkv_counts_to_host.argtypes = [POINTER(Sets), POINTER(c_int32), POINTER(c_int64),
                                            c_void_p]
+    lib.relaxkv_batch_bytes.restype = c_size_t
+    lib.relaxkv_batch_bytes.argtypes = [POINTER(Problem), c_int32, c_int32, c_int32]
+    lib.relaxkv_batch_bind.restype = c_int32
+    lib.relaxkv_batch_bind.argtypes = [POINTER(Problem), c_int32, c_int32, c_int32, c_void_p,
+                                       c_size_t, POINTER(CBatch)]
+    lib.relaxkv_batch_plan.restype = c_int32
+    lib.relaxkv_batch_plan.argtypes = [POINTER(Problem), POINTER(CBatch), c_void_p, c_void_p,
+                                       c_void_p]
+    lib.relaxkv_batch_to_host.restype = c_int32
+    lib.relaxkv_batch_to_host.argtypes = [POINTER(CBatch), POINTER(c_int32), c_void_p]
+    lib.relaxkv_fresh_rows.restype = c_int32
+    lib.relaxkv_fresh_rows.argtypes = [POINTER(Problem), POINTER(CRope), POINTER(CRows), c_void_p,
+                                       c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.relaxkv_batch_rows.restype = c_int32
+    lib.relaxkv_batch_rows.argtypes = [POINTER(Problem), POINTER(CRope), POINTER(CBatch),
+                                       POINTER(CRows), c_void_p, POINTER(CSuffix), c_void_p]
+    lib.relaxkv_shared_attn_workspace_bytes.restype = c_size_t
+    lib.relaxkv_shared_attn_workspace_bytes.argtypes = [POINTER(Problem), POINTER(CBatch)]
+    lib.relaxkv_shared_attn.restype = c_int32
+    lib.relaxkv_shared_attn.argtypes = [POINTER(Problem), POINTER(CBatch), c_int32, c_void_p,
+                                        c_void_p, c_void_p, POINTER(CSuffix), c_void_p, c_void_p,
+                                        c_void_p, c_size_t, c_void_p]
+    lib.relaxkv_block_means.restype = c_int32
+    lib.relaxkv_block_means.argtypes = [POINTER(Problem), c_int32, c_void_p, c_int32, c_void_p,
+                                        c_void_p]
+    lib.relaxkv_block_select_workspace_bytes.restype = c_size_t
+    lib.relaxkv_block_select_workspace_bytes.argtypes = [POINTER(Problem), POINTER(CBatch), c_int32]
+    lib.relaxkv_block_select.restype = c_int32
+    lib.relaxkv_block_select.argtypes = [POINTER(Problem), POINTER(CBatch), c_int32, c_void_p,
+                                         c_void_p, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
+    lib.relaxkv_block_attn_workspace_bytes.restype = c_size_t
+    lib.relaxkv_block_attn_workspace_bytes.argtypes = [POINTER(Problem), POINTER(CBatch), c_int32,
+                                                       c_int32]
+    lib.relaxkv_block_attn.restype = c_int32
+    lib.relaxkv_block_attn.argtypes = [POINTER(Problem), POINTER(CBatch), c_int32, c_void_p,
+                                       c_void_p, c_int32, c_void_p, c_int32, c_void_p,
+                                       POINTER(CSuffix), c_void_p, c_void_p, c_void_p, c_size_t,
+                                       c_void_p]
     _lib = lib
     return lib
 
@@ -444,6 +511,265 @@ class Request:
                                                  _ptr(v_cache), _ptr(k_q), _ptr(v_q), _ptr(out),
                                                  _ptr(lse_out), _stream(stream)),
                "relaxkv_query_attn_noalloc")
+
+    # ---- batched serving: many requests on this request's context cache
+    def alloc_batch(self, n_seq, n_rows, max_suffix):
+        """The maps of a step: n_seq requests with suffixes of up to max_suffix tokens, up to
+        n_rows new tokens in a step."""
+        n_seq, n_rows, max_suffix = int(n_seq), int(n_rows), int(max_suffix)
+        nbytes = self._lib.relaxkv_batch_bytes(self._ref, n_seq, n_rows, max_suffix)
+        if nbytes == 0:
+            raise ValueError(f"no batch of {n_seq} requests, {n_rows} rows and suffixes of "
+                             f"{max_suffix} tokens")
+        buf = torch.zeros(nbytes + 256, dtype=torch.uint8, device=self.device)
+        pad = (-buf.data_ptr()) % 256
+        s = CBatch()
+        _check(self._lib.relaxkv_batch_bind(self._ref, n_seq, n_rows, max_suffix,
+                                            buf.data_ptr() + pad, nbytes, ctypes.byref(s)),
+               "relaxkv_batch_bind")
+        return Batch(self, buf, s, pad)
+
+    def _here(self, stream):
+        """The stream of a batched call, which runs on the request's GPU: the current device
+        has to be that one."""
+        if _current_device is not None and _current_device() != self._index:
+            raise ValueError(f"the request is on {self.device}, the current device is "
+                             f"cuda:{_current_device()}")
+        if stream is not None and stream.device_index != self._index:
+            raise ValueError(f"the stream is not on {self.device}")
+        return _stream(stream)
+
+    def _batch(self, batch):
+        if type(batch) is not Batch or batch.key != (self.T_c, self.H, self.H_kv, self.d, self.dtype,
+                                                     self._index):
+            raise ValueError("batch must come from alloc_batch() of a request of this shape")
+
+    def _suffix(self, batch, k, v):
+        """The suffix caches' descriptor (the library checks the strides)."""
+        shape = (batch.n_seq, self.H_kv, batch.max_suffix, self.d)
+        for t, name in ((k, "k_suffix"), (v, "v_suffix")):
+            if not (type(t) is _Tensor and t.dtype is self.dtype and t.is_cuda
+                    and t.get_device() == self._index and t.shape == shape and t.stride(3) == 1):
+                _need_cache(t, name, self.dtype, shape, self.device)
+        if k.stride() != v.stride() and _cache_strides(k) != _cache_strides(v):
+            raise ValueError("k_suffix and v_suffix must have the same strides")
+        return CSuffix(k.data_ptr(), v.data_ptr(), *_cache_strides(k))
+
+    def _projected(self, t, name, heads, n):
+        """A [n][heads][d] tensor whose rows are contiguous (any row stride); its row stride
+        for the library."""
+        if t is None:
+            return 0
+        if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != self.dtype:
+            raise ValueError(f"{name} must be a {self.dtype} tensor on {self.device}")
+        _need_shape(t, name, (n, heads, self.d))
+        if n and ((heads > 1 and t.stride(1) != self.d) or t.stride(2) != 1):
+            raise ValueError(f"{name} must have contiguous rows")
+        return t.stride(0) if n > 1 else 0
+
+    def _rows(self, q, k, v, n):
+        return CRows(_ptr(q), _ptr(k), _ptr(v), self._projected(q, "q", self.H, n),
+                     self._projected(k, "k", self.H_kv, n), self._projected(v, "v", self.H_kv, n), n)
+
+    def _rope(self, rope):
+        if type(rope) is not Rope:
+            raise ValueError("rope must be a Rope")
+        for t in (rope.inv_freq, rope.q_weight, rope.k_weight):
+            if t is not None and t.device != self.device:
+                raise ValueError(f"rope's tensors must be on {self.device}")
+        for t, name in ((rope.q_weight, "q_weight"), (rope.k_weight, "k_weight")):
+            if t is not None:
+                self._want(t, name, self.dtype, (self.d,))
+        return ctypes.byref(rope.s)
+
+    def plan_batch(self, batch, past_len, new_len, stream=None):
+        """past_len and new_len [n_seq] int32 device: tokens of each request's suffix before
+        the step, and its new tokens."""
+        self._batch(batch)
+        self._want(past_len, "past_len", torch.int32, (batch.n_seq,))
+        self._want(new_len, "new_len", torch.int32, (batch.n_seq,))
+        _check(self._lib.relaxkv_batch_plan(self._ref, batch.ref, past_len.data_ptr(),
+                                            new_len.data_ptr(), self._here(stream)),
+               "relaxkv_batch_plan")
+
+    def fresh_rows(self, rope, positions, q, k, v, q_out, k_out, v_out, stream=None):
+        """Norm and rotation of projected rows at positions [n] int32, values copied: q
+        [n][H][d], k and v [n][H_kv][d] (slices of one fused output, or None) into the dense
+        rows q_out, k_out, v_out of the same shapes."""
+        n = positions.shape[0] if isinstance(positions, torch.Tensor) and positions.dim() == 1 else -1
+        self._want(positions, "positions", torch.int32, (n,))
+        rows = self._rows(q, k, v, n)
+        for t, o, name, heads in ((q, q_out, "q_out", self.H), (k, k_out, "k_out", self.H_kv),
+                                  (v, v_out, "v_out", self.H_kv)):
+            if (t is None) != (o is None):
+                raise ValueError(f"{name} and its input must both be given, or neither")
+            if o is not None:
+                self._want(o, name, self.dtype, (n, heads, self.d))
+        _check(self._lib.relaxkv_fresh_rows(self._ref, self._rope(rope), ctypes.byref(rows),
+                                            positions.data_ptr(), _ptr(q_out), _ptr(k_out),
+                                            _ptr(v_out), self._here(stream)), "relaxkv_fresh_rows")
+
+    def batch_rows(self, rope, batch, q, k, v, q_out, k_suffix, v_suffix, stream=None):
+        """fresh_rows for the rows of a planned step: queries to q_out [n_rows][H][d], keys and
+        values to their tokens of the suffix caches [n_seq][H_kv][max_suffix][d] (any strides
+        with contiguous rows)."""
+        self._batch(batch)
+        n = batch.n_rows
+        rows = self._rows(q, k, v, n)
+        if (q is None) != (q_out is None):
+            raise ValueError("q_out and its input must both be given, or neither")
+        if q_out is not None:
+            self._want(q_out, "q_out", self.dtype, (n, self.H, self.d))
+        suffix = self._suffix(batch, k_suffix, v_suffix)
+        _check(self._lib.relaxkv_batch_rows(self._ref, self._rope(rope), batch.ref,
+                                            ctypes.byref(rows), _ptr(q_out), ctypes.byref(suffix),
+                                            self._here(stream)), "relaxkv_batch_rows")
+
+    def shared_attn_workspace_bytes(self, batch):
+        self._batch(batch)
+        return self._lib.relaxkv_shared_attn_workspace_bytes(self._ref, batch.ref)
+
+    def alloc_shared_workspace(self, batch):
+        n = self.shared_attn_workspace_bytes(batch)
+        return None if n == 0 else torch.empty(n, dtype=torch.uint8, device=self.device)
+
+    def _batch_attn(self, batch, k_cache, v_cache, q, out, lse_out, ws):
+        self._batch(batch)
+        self._caches(k_cache, v_cache)
+        shape = (batch.n_rows, self.H, self.d)
+        self._want(q, "q", self.dtype, shape)
+        self._want(out, "out", self.dtype, shape)
+        if lse_out is not None:
+            self._want(lse_out, "lse_out", torch.float32, shape[:2])
+        if ws is not None:
+            self._ws(ws)
+
+    def shared_attn(self, batch, layer, k_cache, v_cache, q, k_suffix, v_suffix, out, lse_out=None,
+                    ws=None, stream=None):
+        """Attention of a planned step's rows q [n_rows][H][d] over the context cache
+        (k_cache/v_cache as in query_attn) and, causally, their request's suffix
+        [n_seq][H_kv][max_suffix][d], which holds the step's tokens already; out
+        [n_rows][H][d], lse_out [n_rows][H] f32."""
+        self._batch_attn(batch, k_cache, v_cache, q, out, lse_out, ws)
+        suffix = self._suffix(batch, k_suffix, v_suffix)
+        _check(self._lib.relaxkv_shared_attn(self._ref, batch.ref, int(layer), _ptr(k_cache),
+                                             _ptr(v_cache), _ptr(q), ctypes.byref(suffix),
+                                             _ptr(out), _ptr(lse_out), _ptr(ws),
+                                             0 if ws is None else _nbytes(ws), self._here(stream)),
+               "relaxkv_shared_attn")
+
+    # ---- attention over context blocks that a score selects for each row
+    def block_count(self, block):
+        return -(-self.T_c // int(block))
+
+    def block_means(self, layer, k_cache, block, means, stream=None):
+        """Key means over blocks of 16, 32, 64 or 128 positions of one layer of k_cache, or of
+        all of them (layer None): means [n][H_kv][blocks][d]."""
+        self._caches(k_cache, k_cache)
+        if layer is not None and not 0 <= int(layer) < self.L:
+            raise ValueError(f"layer must be None or in [0, {self.L})")
+        if int(block) < 1:
+            raise ValueError("block must be 16, 32, 64 or 128")
+        self._want(means, "means", self.dtype, (self.L if layer is None else 1, self.H_kv,
+                                                self.block_count(block), self.d))
+        _check(self._lib.relaxkv_block_means(self._ref, -1 if layer is None else int(layer),
+                                             _ptr(k_cache), int(block), _ptr(means),
+                                             self._here(stream)), "relaxkv_block_means")
+
+    def block_workspace_bytes(self, batch, block, n_sel):
+        """Scratch of block_select and block_attn (one buffer serves both in turn)."""
+        self._batch(batch)
+        return max(self._lib.relaxkv_block_select_workspace_bytes(self._ref, batch.ref, int(block)),
+                   self._lib.relaxkv_block_attn_workspace_bytes(self._ref, batch.ref, int(block),
+                                                                int(n_sel)))
+
+    def alloc_block_workspace(self, batch, block, n_sel):
+        return torch.empty(self.block_workspace_bytes(batch, block, n_sel), dtype=torch.uint8,
+                           device=self.device)
+
+    def _lists(self, batch, blocks):
+        n = blocks.shape[2] if isinstance(blocks, torch.Tensor) and blocks.dim() == 3 else -1
+        self._want(blocks, "blocks", torch.int32, (batch.n_rows, self.H_kv, n))
+        return n
+
+    def block_select(self, batch, block, means, q, blocks, ws, stream=None):
+        """The context blocks with the largest products of a row's summed group queries and
+        the block means [H_kv][blocks][d] of its layer: blocks [n_rows][H_kv][n_sel] int32,
+        ascending."""
+        self._batch(batch)
+        if int(block) < 1:
+            raise ValueError("block must be 16, 32, 64 or 128")
+        self._want(means, "means", self.dtype, (self.H_kv, self.block_count(block), self.d))
+        self._want(q, "q", self.dtype, (batch.n_rows, self.H, self.d))
+        n_sel = self._lists(batch, blocks)
+        self._ws(ws)
+        _check(self._lib.relaxkv_block_select(self._ref, batch.ref, int(block), _ptr(means), _ptr(q),
+                                              n_sel, _ptr(blocks), _ptr(ws), _nbytes(ws),
+                                              self._here(stream)), "relaxkv_block_select")
+
+    def block_attn(self, batch, layer, k_cache, v_cache, block, blocks, q, k_suffix, v_suffix, out,
+                   lse_out=None, ws=None, stream=None):
+        """shared_attn over the listed blocks of each row and KV head (blocks
+        [n_rows][H_kv][n_sel] int32, entries outside the blocks are none) instead of the whole
+        context."""
+        self._batch_attn(batch, k_cache, v_cache, q, out, lse_out, ws)
+        n_sel = self._lists(batch, blocks)
+        suffix = self._suffix(batch, k_suffix, v_suffix)
+        _check(self._lib.relaxkv_block_attn(self._ref, batch.ref, int(layer), _ptr(k_cache),
+                                            _ptr(v_cache), int(block), _ptr(blocks), n_sel, _ptr(q),
+                                            ctypes.byref(suffix), _ptr(out), _ptr(lse_out),
+                                            _ptr(ws), 0 if ws is None else _nbytes(ws),
+                                            self._here(stream)), "relaxkv_block_attn")
+
+
+class Rope:
+    """Norm and rotation of a model (fresh_rows, batch_rows).
+
+    inv_freq     [rot/2] f32: the angle of pair i at position P is P * inv_freq[i]; rot is a
+                 multiple of 16 up to d (None: no rotation)
+    q_weight, k_weight  [d] in the rows' dtype: RMS norm over each head, None for no norm
+    interleaved  pairs (2i, 2i + 1) instead of (i, i + rot/2)
+    """
+
+    def __init__(self, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
+        if inv_freq is not None and (not isinstance(inv_freq, torch.Tensor)
+                                     or inv_freq.dtype != torch.float32 or inv_freq.dim() != 1
+                                     or not inv_freq.is_contiguous()):
+            raise ValueError("inv_freq must be a contiguous float32 tensor [rot/2]")
+        for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if t is not None and not isinstance(t, torch.Tensor):
+                raise ValueError(f"{name} must be a tensor or None")
+        self.inv_freq, self.q_weight, self.k_weight = inv_freq, q_weight, k_weight
+        self.s = CRope(_ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), float(eps),
+                       0 if inv_freq is None else 2 * inv_freq.shape[0], 1 if interleaved else 0)
+
+
+class Batch:
+    """Device arrays of relaxkv_batch (views into one torch buffer)."""
+
+    def __init__(self, req, buf, s, pad):
+        self.buf, self.s, self.ref = buf, s, ctypes.byref(s)
+        self.n_seq, self.n_rows, self.max_suffix = s.n_seq, s.n_rows, s.max_suffix
+        self.key = (req.T_c, req.H, req.H_kv, req.d, req.dtype, req._index)
+        base = buf.data_ptr()
+
+        def view(ptr, n):
+            off = ptr - base
+            return buf[off:off + 4 * n].view(torch.int32)
+
+        self.row_off = view(s.row_off, s.n_seq + 1)
+        self.row_seq = view(s.row_seq, s.n_rows)
+        self.row_pos = view(s.row_pos, s.n_rows)
+        self.counts = view(s.counts, 4)
+
+    def counts_to_host(self, stream=None, check=True):
+        """[rows, row tiles, 0, error word] of the planned step on the host; synchronises the
+        stream.  With check=True a set error word raises RelaxKVError."""
+        c = (c_int32 * 4)()
+        st = load().relaxkv_batch_to_host(self.ref, c, _stream(stream))
+        if check or st not in (OK, EINVAL):
+            _check(st, "relaxkv_batch_to_host")
+        return list(c)
 
 
 class SetsBuffer:
