@@ -513,7 +513,8 @@ relaxkv_status relaxkv_counts_to_host(const relaxkv_sets* s, int32_t* host_count
  *   row_seq  [n_rows]   request of each row, -1 behind the step's last row.
  *   row_pos  [n_rows]   position T_c + past_b + i of each row, -1 behind the last.
  *   tiles    [tile_cap][8]  the attention's row tiles (internal).
- *   counts   [4]        rows of the step, row tiles, 0, error word.
+ *   counts   [64]       rows of the step, row tiles, tokens of the longest suffix that a row
+ *                       sees, error word; the rest is internal.
  * T_c, H, H_kv, d and dtype are those of the problem the batch was bound for; every call
  * refuses a batch of another shape.
  */
@@ -632,8 +633,9 @@ size_t relaxkv_shared_attn_workspace_bytes(const relaxkv_problem* p, const relax
  *             natural-log normaliser.  Rows behind the step's last are left as they are.
  *   ws        device scratch of ws_bytes >= relaxkv_shared_attn_workspace_bytes(p, b); two
  *             calls that share it must be ordered.
- * The same call gives the same bits on every run; the last bits depend on n_rows, n_seq,
- * max_suffix and T_c, which choose the splits.
+ * The same call gives the same bits on every run.  The last bits of a row depend on the
+ * step's number of rows, row tiles and longest suffix, which choose the splits, but not on
+ * the room of the batch (n_rows, max_suffix).
  */
 relaxkv_status relaxkv_shared_attn(const relaxkv_problem* p, const relaxkv_batch* b, int32_t layer,
                                    const void* k_cache, const void* v_cache, const void* q,

@@ -28,19 +28,80 @@ struct alignas(16) BatchTile {
     int32_t row0, pad[3];
 };
 
-// Scratch of the bf16 batched attention: per key split, KV head and (token, head) row the
-// unnormalised output (float32) and (running max, sum of the rounded probabilities, sum of
-// the exact ones, -).
-struct BatchAttnWorkspace {
-    size_t part_s_off;  // float4 [n_ctx + n_suf][H_kv][n_rows * G]; the outputs lie at 0
-    size_t total;
-    int n_ctx, kps;     // splits of the context keys (listed keys for the blocks), keys each
-    int n_suf, kss;     // splits of the suffix keys, keys each
-    int n_chunks;       // row chunks of kBatchRowsBf16 (of all rows; of one token's group)
+// How the bf16 attention of a step is split, computed by the plan (which knows the step) and
+// kept behind the public counts.
+constexpr int kBaRows = kBatchRowsBf16;
+constexpr int kBaKeys = 32;            // keys per tile
+constexpr int kBaWgs = 768;            // workgroups the splits aim for (three per CU)
+constexpr int kBaMinTiles = 8;         // fewest tiles per split
+constexpr int kBaXcds = 8;
+constexpr int kBatchSplitAt = 16;      // first word of the split in relaxkv_batch::counts
+
+// Shared context: item (g, chunk) = g * chunks + chunk holds `tiles` key tiles, worker w takes
+// the tiles [w * quota, (w + 1) * quota) of the items laid one after another.  Where every item
+// gets several workers, the items are padded to a whole number of quotas (len), so a worker
+// has one item and the chunks of a key range run side by side on one XCD, whose L2 then
+// serves all but the first (64 decoding requests over 32K: 32 workers per item).  With fewer
+// workers per item the padding would idle a large part of them (20 ragged questions over 8K: 4
+// per item), so there the workers cut the items anywhere, one worker's range covering
+// parts of several.
+struct BatchSplit {
+    int32_t rows, row_tiles;           // of the step
+    int32_t chunks, items, tiles, len, quota, workers;
+    int32_t per_item;                  // workers of an item; 0: cut anywhere
+    int32_t suf_n, suf_kps;            // suffix splits, keys each
 };
 
-BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_batch& b, int block,
-                                     int n_sel);
+// Splits n of `tiles` key tiles, `quota` tiles each, so that `items` of them fill the chip.
+__host__ __device__ inline void batch_split_keys(int tiles, int items, int& n, int& quota) {
+    const int want = items >= kBaWgs ? 1 : kBaWgs / (items > 0 ? items : 1);
+    quota = (tiles + want - 1) / want;
+    quota = quota < kBaMinTiles ? kBaMinTiles : quota;
+    n = tiles > 0 ? (tiles + quota - 1) / quota : 1;
+}
+
+__host__ __device__ inline BatchSplit batch_split(int rows, int row_tiles, int longest, int T, int G,
+                                                  int Hkv) {
+    BatchSplit s;
+    s.rows = rows;
+    s.row_tiles = row_tiles;
+    s.chunks = (rows * G + kBaRows - 1) / kBaRows;
+    s.items = s.chunks * Hkv;
+    s.tiles = (T + kBaKeys - 1) / kBaKeys;
+    const int most = (s.tiles + kBaMinTiles - 1) / kBaMinTiles;
+    int n = s.items > 0 ? kBaWgs / s.items : 0;
+    n = n < most ? n : most;
+    // (whole rounds of the XCDs)
+    while (n > 0 && (n * Hkv + kBaXcds - 1) / kBaXcds * kBaXcds * s.chunks > kBaWgs) --n;
+    s.per_item = n >= 6 || n == most ? n : 0;
+    if (s.per_item) {
+        s.quota = (s.tiles + n - 1) / n;
+        s.len = n * s.quota;
+        s.workers = s.items * n;
+    } else {
+        const int64_t all = (int64_t)s.items * s.tiles;
+        const int64_t q = (all + kBaWgs - 1) / kBaWgs;
+        s.quota = q < kBaMinTiles ? kBaMinTiles : (int32_t)q;
+        s.len = s.tiles;
+        s.workers = (int32_t)((all + s.quota - 1) / s.quota);
+    }
+    int quota;
+    batch_split_keys((longest + kBaKeys - 1) / kBaKeys, row_tiles * Hkv, s.suf_n, quota);
+    s.suf_kps = quota * kBaKeys;
+    return s;
+}
+
+// Scratch of the bf16 batched attention: partial rows of fp16 outputs, and 16 bytes of
+// statistics each; those of the suffix items follow the context's.
+struct BatchAttnWorkspace {
+    size_t part_s_off;  // the statistics; the outputs lie at 0
+    size_t total;
+    size_t suf_part;    // first partial row of the suffix items
+    int ctx_wgs, suf_wgs;
+};
+
+// n_sel = 0: the whole context.
+BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_batch& b, int n_sel);
 size_t block_select_bytes(const relaxkv_problem& p, const relaxkv_batch& b, int block);
 
 inline int block_count(const relaxkv_problem& p, int block) { return (p.T_c + block - 1) / block; }

@@ -6,22 +6,25 @@
 //
 // bf16: one launch of independent work items, then a merge.
 // - Context items.  Shared: the (token, head) rows of ALL requests of a KV head in chunks of
-//   128, times one split of the keys, so K and V are read once for the batch and not
-//   once per request.  The chunks of one split are consecutive on one XCD, whose L2 then
-//   serves all but the first.  Listed: one token's group of heads, times one split of its
-//   listed keys; the list is first compacted into LDS (full blocks, then copies of a
-//   partial last block), so that every key below the count is one the row sees.
+//   128, over key tiles, so K and V are read once for the batch and not once per request.
+//   Listed: one token's group of heads, times one split of its listed keys; the list is
+//   first compacted into LDS (full blocks, then copies of a partial last block), so that
+//   every key below the count is one the row sees.
 // - Suffix items: 128 rows of one request, times one split of its keys, causal.
-// - Each item streams 64-key K and V tiles through two swizzled LDS buffers by direct loads;
-//   64 KB of LDS let two workgroups share a CU, so that one's softmax and waits overlap
-//   the other's matrix products.  A wave owns 32 rows (one per lane): S^T = K Q^T, online
+// - How the items are split over workgroups (BatchSplit) follows from the step itself and
+//   comes with its plan, so a batch with room for many rows costs a small step nothing.
+// - Each item streams 32-key K and V tiles through three swizzled LDS buffers by direct
+//   loads; 48 KB of LDS and 163 registers let three workgroups share a CU, whose softmax,
+//   matrix products and waits overlap.  A wave owns 32 rows (one per lane): S^T = K Q^T, online
 //   softmax in the exp2 domain with a lazily raised maximum, O^T += V^T P^T.
 // - Probabilities are rounded to bf16 for the second product (2^-9 of each, independent over
-//   keys: about as much as rounding O once; fp32 products would take eight times the matrix
+//   keys: about as much as rounding O once; float32 products would take eight times the matrix
 //   time).  The output is divided by the sum of the rounded ones, which keeps a row that
 //   sees one key exact, the log-sum-exp uses the sum of the exact ones.
-// - Every item writes its unnormalised float32 output and (max, sums); batch_merge adds them
-//   with weights exp2(max_s - max) in a fixed order.
+// - Every item writes its unnormalised output and (max, sums, scale); batch_merge adds them
+//   with weights exp2(max_s - max) in a fixed order.  The outputs are written as fp16 over
+//   the row's largest element (2^-12 of an element, an eighth of what rounding O to bf16 costs,
+//   for half the traffic of float32).
 // A row that sees no key gets O = 0 and lse = -inf.
 // Loads never leave a run's keys (past its end they repeat its last key, masked), so cache
 // rows past the context and suffix tokens past a request's length are never read.
@@ -38,14 +41,12 @@
 namespace relaxkv {
 namespace {
 
-constexpr int kBaKeys = 64;            // keys per tile
-constexpr int kBaStages = 2;           // LDS ring depth
+constexpr int kBaStages = 3;           // LDS ring depth
 constexpr int kBaWaves = kBatchRowsBf16 / 32;
 constexpr int kBaRing = 4;             // K fragments read ahead of their MFMA
+constexpr int kBaRingV = 4;            // and V fragments
 constexpr float kBaSlack = 8.0f;       // log2 units the running max may lag the true max
-constexpr long kBaWgs = 512;           // workgroups the key splits aim for (two per CU)
-constexpr long kBaMinSplit = 256;      // fewest keys per split
-constexpr int kBaXcds = 8;
+constexpr float kBaHuge = 1 << 20;     // log2 units from which half an ulp is near 2^-4
 
 template <int N> struct Int { static constexpr int value = N; };
 
@@ -58,14 +59,36 @@ struct BaArgs {
     const uint16_t *ks, *vs; // suffixes: key i of request b at b * s_ss + g * s_sh + i * s_st
     int64_t c_sh, c_st, s_ss, s_sh, s_st;
     const int32_t* counts;
+    const int32_t* row_pos;
     const BatchTile* tiles;
     const int32_t* lists;    // [n_rows][Hkv][n_sel]
-    float* part_o;           // [slot][Hkv][n_rows * G][D]
-    float4* part_s;          // [slot][Hkv][n_rows * G]
+    // Partial rows: context ones first (shared: kBaRows per segment; listed: [split][Hkv][rows of
+    // the step]), suffix ones ([split][Hkv][rows of the step]) from suf_part.
+    _Float16* part_o;
+    float4* part_s;          // (max, sum of rounded, sum of exact probabilities, scale)
+    size_t suf_part;
     int T, H, Hkv, G, n_rows, n_sel, bshift, nb, tail;
-    int n_ctx, kps, n_suf, kss, n_chunks, ctx_items;
+    int ctx_wgs;             // context workgroups of the launch; the others take suffix items
+    int list_tiles, list_items;   // listed: key tiles of a row at most, items of a token
     float sl2;               // softmax scale * log2(e)
 };
+
+// The step's split, through the scalar cache (it was written by an earlier kernel).
+__device__ __forceinline__ BatchSplit load_split(const int32_t* counts) {
+    typedef const __attribute__((address_space(4))) int32_t const_word;
+    struct Words { int32_t w[sizeof(BatchSplit) / 4]; } words;
+    const_word* p = (const_word*)(uintptr_t)(counts + kBatchSplitAt);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(BatchSplit) / 4); ++i) words.w[i] = p[i];
+    return __builtin_bit_cast(BatchSplit, words);
+}
+
+// Listed keys of a row: splits, keys of each.
+__device__ __forceinline__ void list_split(const BaArgs& a, int rows, int& n, int& kps) {
+    const int tiles = a.list_tiles;
+    batch_split_keys(tiles, rows * a.list_items, n, kps);
+    kps *= kBaKeys;
+}
 
 __device__ __forceinline__ float ba_pair_max(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -114,73 +137,100 @@ __device__ __forceinline__ int list_key(int c, const int* lst, int nf, int bshif
 }
 
 template <int D, bool LIST>
-__global__ __launch_bounds__(kBaWaves * 64, 2) void battn_bf16(BaArgs a) {
+__global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
     constexpr int TK = kBaKeys, ST = kBaStages, NW = kBaWaves;
     constexpr int KS = D / 16;             // k-steps of QK^T
     constexpr int DB = D / 32;             // 32-wide d blocks of O^T
-    constexpr int NKB = TK / 32;
     constexpr int ROWB = 2 * D;            // tile row bytes
     constexpr int CH = D / 8;              // 16-byte chunks per row
     constexpr int RPI = 64 / CH;           // rows per wave-wide load
     constexpr int NL = TK / RPI;           // wave-wide loads per tile and tensor
     constexpr int NI = NL / NW;            // of them per wave
     constexpr int LPW = 2 * NI;            // K and V
-    static_assert(NL % NW == 0, "loader shape");
-    __shared__ __attribute__((aligned(1024))) uint16_t Kt[ST][TK * D];
-    __shared__ __attribute__((aligned(1024))) uint16_t Vt[ST][TK * D];
-    __shared__ int lst[LIST ? RELAXKV_MAX_SELECTED_BLOCKS : 1], cnt[2];
+    static_assert(NL % NW == 0 && TK == 32 && ST == 3, "tile shape");
+    __shared__ __attribute__((aligned(1024))) uint16_t tiles[2 * ST * TK * D];   // K, then V
+    extern __shared__ int lst[];                         // listed: n_sel blocks
+    __shared__ int cnt[2];
 
-    const int tid = threadIdx.x, lane = tid & 63, r32 = lane & 31, hf = lane >> 5;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int id = blockIdx.x;
-    const int rows = min(a.counts[0], a.n_rows);
-    const bool ctx = id < a.ctx_items;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool ctx = (int)blockIdx.x < a.ctx_wgs;
+    const BatchSplit sp = load_split(a.counts);
+    const size_t R = (size_t)sp.rows * a.G;              // rows of the step per KV head
 
-    // The item: KV head g, partial slot, the lane's row (token t, head hh of the group, last
-    // visible key lim), and its keys key0 .. key0 + nk - 1 of a run (base pointers, stride).
-    int g, slot, t, hh, lim, key0, nk, open;             // open: keys that every row sees
-    bool valid;
+    // Shared context: the worker's tiles x .. x_end - 1.
+    int worker = 0;
+    int64_t x = 0, x_end = 0;
+    if (sp.rows == 0) return;
+    if (ctx && !LIST) {
+        const int j = blockIdx.x / kBaXcds, xcd = blockIdx.x % kBaXcds;
+        if (sp.per_item) {
+            // (the chunks of one key range are consecutive workgroups of one XCD)
+            const int pair = j / sp.chunks * kBaXcds + xcd;
+            if (pair >= sp.per_item * a.Hkv) return;
+            worker = (pair % a.Hkv * sp.chunks + j % sp.chunks) * sp.per_item + pair / a.Hkv;
+        } else {
+            worker = xcd * (kBaWgs / kBaXcds) + j;       // (neighbours share an XCD)
+        }
+        if (worker >= sp.workers) return;
+        x = (int64_t)worker * sp.quota;
+        x_end = min(x + sp.quota, (int64_t)sp.items * sp.len);
+    }
+
+  for (;;) {
+    // Made opaque per item, so that what is derived from it is not kept live across the loop.
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int r32 = lane & 31, hf = lane >> 5;
+    // The item: KV head g, the wave's first partial row and number of rows (consecutive ones),
+    // the lane's row (token t, head hh of the group, last visible key lim), and the keys key0 ..
+    // key0 + nk - 1 of a run (base pointers, stride); the first `open` of them every row sees.
+    int g, t, hh, lim, key0, nk, open, n_val;
     const uint16_t *kb, *vb;
     int64_t st;
+    size_t part;
     bool listed = false;
     if (ctx) {
         if constexpr (LIST) {
-            slot = id % a.n_ctx;
-            int x = id / a.n_ctx;
-            const int chunk = x % a.n_chunks;
-            x /= a.n_chunks;
-            g = x % a.Hkv;
-            t = x / a.Hkv;
-            if (t >= rows) return;
+            int y = blockIdx.x, list_n, list_kps;
+            list_split(a, sp.rows, list_n, list_kps);
+            const int split = y % list_n;
+            y /= list_n;
+            int chunk = 0;
+            if (a.G > kBaRows) {
+                const int chunks = (a.G + kBaRows - 1) / kBaRows;
+                chunk = y % chunks;
+                y /= chunks;
+            }
+            g = y % a.Hkv;
+            t = y / a.Hkv;
+            if (t >= sp.rows) return;
             compact_list(a.lists + ((size_t)t * a.Hkv + g) * a.n_sel, a.n_sel, a.nb, a.tail, lst, cnt);
-            hh = chunk * kBatchRowsBf16 + w * 32 + r32;
-            valid = hh < a.G;
-            if (!valid) hh = 0;
-            key0 = slot * a.kps;
+            const int h0 = chunk * kBaRows + w * 32;
+            n_val = a.G - h0;
+            hh = r32 < n_val ? h0 + r32 : 0;
+            part = ((size_t)split * a.Hkv + g) * R + (size_t)t * a.G + h0;
+            key0 = split * list_kps;
             const int n = __builtin_amdgcn_readfirstlane((cnt[0] << a.bshift) + cnt[1] * a.tail);
-            nk = min(a.kps, n - key0);
+            nk = min(list_kps, n - key0);
             if (nk <= 0) {                               // nothing in this split
-                if (valid && hf == 0)
-                    a.part_s[((size_t)slot * a.Hkv + g) * ((size_t)a.n_rows * a.G) + (size_t)t * a.G + hh] =
-                        float4{-INFINITY, 0.f, 0.f, 0.f};
+                if (lane < min(n_val, 32)) a.part_s[part + lane] = float4{-INFINITY, 0.f, 0.f, 0.f};
                 return;
             }
             listed = true;
         } else {
-            // (the chunks of one (split, head) pair are consecutive workgroups of one XCD)
-            const int x = id / kBaXcds, chunk = x % a.n_chunks;
-            const int pair = x / a.n_chunks * kBaXcds + id % kBaXcds;
-            if (pair >= a.n_ctx * a.Hkv) return;
-            g = pair % a.Hkv;
-            slot = pair / a.Hkv;
-            const int row0 = chunk * kBatchRowsBf16;
-            if (row0 >= rows * a.G) return;
-            const int rho = row0 + w * 32 + r32;
-            valid = rho < rows * a.G;
-            t = valid ? rho / a.G : 0;
-            hh = valid ? rho - t * a.G : 0;
-            key0 = slot * a.kps;
-            nk = min(a.kps, a.T - key0);
+            const int item = (int)(x / sp.len), t0 = (int)(x - (int64_t)item * sp.len);
+            const int left = (int)(x_end - x), nt = min(left, sp.tiles - t0);
+            x += min(left, sp.len - t0);                 // (the next item's first tile)
+            if (nt <= 0) return;                         // (padding, which ends a range)
+            g = item / sp.chunks;
+            const int rho0 = (item - g * sp.chunks) * kBaRows + w * 32;
+            n_val = sp.rows * a.G - rho0;
+            const int rho = r32 < n_val ? rho0 + r32 : 0;
+            t = rho / a.G;
+            hh = rho - t * a.G;
+            part = (size_t)(worker + item) * kBaRows + w * 32;
+            key0 = t0 * TK;
+            nk = min(nt * TK, a.T - key0);
         }
         lim = nk - 1;
         open = nk;
@@ -188,38 +238,38 @@ __global__ __launch_bounds__(kBaWaves * 64, 2) void battn_bf16(BaArgs a) {
         vb = a.vc + g * a.c_sh;
         st = a.c_st;
     } else {
-        int x = id - a.ctx_items;
-        const int split = x % a.n_suf;
-        x /= a.n_suf;
-        g = x % a.Hkv;
-        x /= a.Hkv;
-        const int n_tiles = a.counts[1];
-        BatchTile tl = a.tiles[x];                       // (tiles past the count: unspecified)
-        if (x >= n_tiles) return;
+        int y = blockIdx.x - a.ctx_wgs;
+        const int split = y % sp.suf_n;
+        y /= sp.suf_n;
+        g = y % a.Hkv;
+        y /= a.Hkv;
+        if (y >= sp.row_tiles) return;
+        BatchTile tl = a.tiles[y];
         tl.seq = __builtin_amdgcn_readfirstlane(tl.seq);
         tl.row_begin = __builtin_amdgcn_readfirstlane(tl.row_begin);
         tl.n_new = __builtin_amdgcn_readfirstlane(tl.n_new);
         tl.past = __builtin_amdgcn_readfirstlane(tl.past);
         tl.row0 = __builtin_amdgcn_readfirstlane(tl.row0);
-        slot = a.n_ctx + split;
-        key0 = split * a.kss;
+        key0 = split * sp.suf_kps;
         const int n_th = tl.n_new * a.G;                 // (token, head) rows of the request
-        const int last = (min(tl.row0 + kBatchRowsBf16, n_th) - 1) / a.G;
-        nk = min(a.kss, tl.past + last + 1 - key0);
+        const int last = (min(tl.row0 + kBaRows, n_th) - 1) / a.G;
+        nk = min(sp.suf_kps, tl.past + last + 1 - key0);
         if (nk <= 0) return;
-        const int rq = tl.row0 + w * 32 + r32;
-        valid = rq < n_th;
-        const int tr = valid ? rq / a.G : 0;
-        hh = valid ? rq - tr * a.G : 0;
+        const int rq0 = tl.row0 + w * 32;
+        n_val = n_th - rq0;
+        const int rq = r32 < n_val ? rq0 + r32 : 0;
+        const int tr = rq / a.G;
+        hh = rq - tr * a.G;
         t = tl.row_begin + tr;
-        lim = tl.past + tr - key0;
+        part = a.suf_part + ((size_t)split * a.Hkv + g) * R + (size_t)tl.row_begin * a.G + rq0;
+        lim = tl.past + tr - key0;                       // (below 0: the merge skips the split)
         open = min(nk, tl.past + tl.row0 / a.G + 1 - key0);
-        valid = valid && lim >= 0;                       // (the merge reads no others)
         kb = a.ks + tl.seq * a.s_ss + g * a.s_sh;
         vb = a.vs + tl.seq * a.s_ss + g * a.s_sh;
         st = a.s_st;
     }
-    const bool live = __any(valid);
+    const bool live = n_val > 0;
+    const int lim4 = lim - 4 * hf;
     const int ntile = (nk + TK - 1) / TK;
 
     bf16x8 qf[KS];
@@ -234,7 +284,8 @@ __global__ __launch_bounds__(kBaWaves * 64, 2) void battn_bf16(BaArgs a) {
     f32x16 o[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = f32x16{};
-    float m_run = -INFINITY, l_run = 0.f, l_exact = 0.f;
+    // The row's reference maximum, what the logits are compared with, and subtracted from them.
+    float m_run = -INFINITY, thr = -INFINITY, m_ref = 0.f, l_run = 0.f, l_exact = 0.f;
 
     // Loader: load jj = w + NW i fills tile rows jj RPI ..; lane l writes (row l / CH, chunk
     // l % CH) and fetches the chunk that belongs there.  The swizzle of a lane's rows is the
@@ -244,16 +295,16 @@ __global__ __launch_bounds__(kBaWaves * 64, 2) void battn_bf16(BaArgs a) {
     static_assert((NW * RPI) % 16 == 0, "the swizzle repeats every 16 rows");
     const int ch8 = (pchunk ^ tile_swz<D>(w * RPI + lrow)) << 3;
     const uint32_t lane_off = (uint32_t)(lrow * (int)st + ch8) * 2u;
-    const uint32_t kt0 = lds_addr(Kt[0]) + w * RPI * ROWB, vt0 = lds_addr(Vt[0]) + w * RPI * ROWB;
+    const uint32_t kt0 = lds_addr(tiles) + w * RPI * ROWB, vt0 = kt0 + ST * TK * ROWB;
     auto issue = [&](int tt) {
         const uint32_t so = (uint32_t)(tt % ST) * (TK * ROWB);
         if (!listed && (tt + 1) * TK <= nk) {
             const int64_t e0 = (int64_t)(key0 + tt * TK + w * RPI) * st;
-            const uint16_t *kp = kb + e0, *vp = vb + e0;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
-                fill_lds16_u(kp + (int64_t)(NW * RPI * i) * st, lane_off, kt0 + so + i * (NW * RPI * ROWB));
-                fill_lds16_u(vp + (int64_t)(NW * RPI * i) * st, lane_off, vt0 + so + i * (NW * RPI * ROWB));
+                const int64_t e = e0 + (int64_t)(NW * RPI * i) * st;
+                fill_lds16_u(kb + e, lane_off, kt0 + so + i * (NW * RPI * ROWB));
+                fill_lds16_u(vb + e, lane_off, vt0 + so + i * (NW * RPI * ROWB));
             }
         } else {
 #pragma unroll
@@ -274,52 +325,59 @@ __global__ __launch_bounds__(kBaWaves * 64, 2) void battn_bf16(BaArgs a) {
     const int cl = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
     const int v_base0 = rl * ROWB | ((cl ^ tile_swz<D>(rl)) << 4) | ((lane & 1) << 3);
     const int v_base1 = (rl + 8) * ROWB | ((cl ^ tile_swz<D>(rl + 8)) << 4) | ((lane & 1) << 3);
-    const char* kst = (const char*)Kt[0];
-    const uint32_t vlds = lds_addr(Vt[0]);
+    const char* kst = (const char*)tiles;
+    const uint32_t vlds = lds_addr(tiles) + ST * TK * ROWB;
 
-    auto step = [&](uint32_t stage, int c0, bool masked) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    auto step = [&](uint32_t stage, int c0) {
         int kbo = k_base + (int)stage;
         uint32_t vb0 = v_base0 + vlds + stage, vb1 = v_base1 + vlds + stage;
         asm volatile("" : "+v"(kbo), "+v"(vb0), "+v"(vb1));
-        // S^T = K Q^T: s[kb][v] = S[row][key c0 + 32kb + 8(v/4) + 4hf + v%4]
-        f32x16 s[NKB];
-#pragma unroll
-        for (int kb = 0; kb < NKB; ++kb) s[kb] = f32x16{};
-        auto frag = [&](int x) {                       // x = NKB ks + kb
-            return *(const bf16x8*)(kst + (x % NKB) * 32 * ROWB + (kbo ^ ((x / NKB) << 5)));
-        };
+        // S^T = K Q^T: s[v] = S[row][key c0 + 8(v/4) + 4hf + v%4]
+        f32x16 s;
+        auto frag = [&](int x) { return *(const bf16x8*)(kst + (kbo ^ (x << 5))); };
         bf16x8 kf[kBaRing];
 #pragma unroll
         for (int i = 0; i < kBaRing; ++i) kf[i] = frag(i);
 #pragma unroll
-        for (int x = 0; x < NKB * KS; ++x) {
+        for (int x = 0; x < KS; ++x) {
             const bf16x8 cur = kf[x % kBaRing];
-            if (x + kBaRing < NKB * KS) kf[x % kBaRing] = frag(x + kBaRing);
-            s[x % NKB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cur, qf[x / NKB], s[x % NKB], 0, 0, 0);
+            if (x + kBaRing < KS) kf[x % kBaRing] = frag(x + kBaRing);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cur, qf[x], x == 0 ? f32x16{} : s, 0, 0, 0);
         }
+        // V fragments, the first ones read ahead of the softmax: y = 2 db + k2
+        auto vfrag = [&](int y) {
+            const uint32_t rowo = (y & 1) * 16 * ROWB;
+            const v4i16 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_v4i16*)(uintptr_t)((vb0 ^ (y / 2 << 6)) + rowo));
+            const v4i16 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_v4i16*)(uintptr_t)((vb1 ^ (y / 2 << 6)) + rowo));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        bf16x8 vf[kBaRingV];
+#pragma unroll
+        for (int i = 0; i < kBaRingV; ++i) vf[i] = vfrag(i);
         __builtin_amdgcn_sched_group_barrier(0x100, kBaRing, 0);
 #pragma unroll
-        for (int x = 0; x < NKB * KS; ++x) {
+        for (int x = 0; x < KS; ++x) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (x + kBaRing < NKB * KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (x + kBaRing < KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            else __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
-        if (masked) {                                  // the run's tail, or the causal future
-            const int e = lim - c0 - 4 * hf;
+        if (c0 + TK > open) {                          // the run's tail, or the causal future
+            const int e = lim4 - c0;
 #pragma unroll
-            for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (32 * kb + 8 * (v >> 2) + (v & 3) > e) s[kb][v] = -INFINITY;
+            for (int v = 0; v < 16; ++v)
+                if (8 * (v >> 2) + (v & 3) > e) s[v] = -INFINITY;
         }
-        float mk[NKB];
+        float mk = fmaxf(s[0], s[1]), mk2 = fmaxf(s[2], s[3]);
 #pragma unroll
-        for (int kb = 0; kb < NKB; ++kb) {
-            mk[kb] = fmaxf(s[kb][0], s[kb][1]);
-#pragma unroll
-            for (int v = 2; v < 16; v += 2) mk[kb] = fmaxf(fmaxf(mk[kb], s[kb][v]), s[kb][v + 1]);
+        for (int v = 4; v < 16; v += 4) {
+            mk = fmaxf(fmaxf(mk, s[v]), s[v + 1]);
+            mk2 = fmaxf(fmaxf(mk2, s[v + 2]), s[v + 3]);
         }
-        const float mx = ba_pair_max(fmaxf(mk[0], mk[NKB - 1])) * a.sl2;
-        if (__any(mx > m_run + kBaSlack)) {
+        const float mx = ba_pair_max(fmaxf(mk, mk2)) * a.sl2;
+        if (__any(mx > thr)) {
             const float m_new = mx > m_run + kBaSlack ? mx : m_run;
             const float alpha = m_new == m_run ? 1.f : fast_exp2(m_run - m_new);
             l_run *= alpha;
@@ -327,118 +385,194 @@ __global__ __launch_bounds__(kBaWaves * 64, 2) void battn_bf16(BaArgs a) {
 #pragma unroll
             for (int db = 0; db < DB; ++db) o[db] *= alpha;
             m_run = m_new;
-        }
-        // (a row with no visible key so far adds exact zeros)
-        const float m_ref = m_run == -INFINITY ? 0.f : m_run;
-        bf16x8 pb[NKB][2];
-        float e0 = 0.f, e1 = 0.f, e2 = 0.f, e3 = 0.f;
+            // The maximum is rounded, the product in the multiply-add below is not: where
+            // logits are huge (a split of keys at the type's lowest value), what the rounding
+            // cut off would be an exponent of its own.  Such a row enters here for every tile, has
+            // the product rounded too and its logits moved to a maximum of 0.
+            const bool none = m_run == -INFINITY, huge = !none && fabsf(m_run) > kBaHuge;
+            m_ref = none || huge ? 0.f : m_run;          // (no visible key so far: exact zeros)
+            thr = huge ? -INFINITY : m_run + kBaSlack;
+            if (__any(huge)) {
 #pragma unroll
-        for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const float p = fast_exp2(fmaf(s[kb][v], a.sl2, -m_ref));
-                ((v & 3) == 0 ? e0 : (v & 3) == 1 ? e1 : (v & 3) == 2 ? e2 : e3) += p;
-                pb[kb][v >> 3][v & 7] = (__bf16)p;
-            }
-        l_exact += (e0 + e1) + (e2 + e3);
-        {
-            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-            const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
-            float ls0 = 0.f, ls1 = 0.f, ls2 = 0.f, ls3 = 0.f;
-#pragma unroll
-            for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-                for (int k2 = 0; k2 < 2; ++k2) {
-                    const bf16x8 q8 = pb[kb][k2];
-                    ls0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 0, 1), one2, ls0, false);
-                    ls1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 2, 3), one2, ls1, false);
-                    ls2 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 4, 5), one2, ls2, false);
-                    ls3 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 6, 7), one2, ls3, false);
+                for (int v = 0; v < 16; ++v) {
+                    float x = s[v] * a.sl2;
+                    asm volatile("" : "+v"(x));          // (not a multiply-add)
+                    s[v] = huge ? (x - m_run) * (1.0f / a.sl2) : s[v];
                 }
-            l_run += (ls0 + ls1) + (ls2 + ls3);
+            }
         }
+        bf16x8 pb[2];
+        float e0 = 0.f, e1 = 0.f;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const float p = fast_exp2(fmaf(s[v], a.sl2, -m_ref));
+            (v & 1 ? e1 : e0) += p;
+            pb[v >> 3][v & 7] = (__bf16)p;
+        }
+        l_exact += e0 + e1;
+        const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
+        float ls0 = 0.f, ls1 = 0.f;
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+            const bf16x8 q8 = pb[k2];
+            ls0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 0, 1), one2, ls0, false);
+            ls1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 2, 3), one2, ls1, false);
+            ls0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 4, 5), one2, ls0, false);
+            ls1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 6, 7), one2, ls1, false);
+        }
+        l_run += ls0 + ls1;
         // O^T += V^T P^T
 #pragma unroll
-        for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int k2 = 0; k2 < 2; ++k2) {
-                    const uint32_t rowo = (kb * 32 + k2 * 16) * ROWB;
-                    const v4i16 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_v4i16*)(uintptr_t)((vb0 ^ (db << 6)) + rowo));
-                    const v4i16 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_v4i16*)(uintptr_t)((vb1 ^ (db << 6)) + rowo));
-                    const bf16x8 vv = __builtin_bit_cast(
-                        bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, pb[kb][k2], o[db], 0, 0, 0);
-                }
+        for (int y = 0; y < 2 * DB; ++y) {
+            const bf16x8 cur = vf[y % kBaRingV];
+            if (y + kBaRingV < 2 * DB) vf[y % kBaRingV] = vfrag(y + kBaRingV);
+            o[y / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cur, pb[y & 1], o[y / 2], 0, 0, 0);
+        }
     };
 
 #pragma unroll
     for (int tt = 0; tt < ST - 1; ++tt)
         if (tt < ntile) issue(tt);
     for (int tt = 0; tt < ntile; ++tt) {
-        // Tile tt has landed, and every wave is done with the buffer that is filled next.
-        wait_loads_barrier<0>();
+        // Tile tt has landed (the later one of the ring may be in flight), and every wave is done
+        // with the buffer that is filled next.
+        if (tt + 1 < ntile) wait_loads_barrier<LPW>();
+        else wait_loads_barrier<0>();
         if (tt + ST - 1 < ntile) issue(tt + ST - 1);
-        if (live) step((uint32_t)(tt % ST) * (TK * ROWB), tt * TK, (tt + 1) * TK > open);
+        if (live) step((uint32_t)(tt % ST) * (TK * ROWB), tt * TK);
     }
 
+    // The partial rows: scaled by the largest finite element, transposed through LDS (the
+    // tiles are done with) and written as whole rows.
     const float l_tot = ba_pair_sum(l_run), l_ex = ba_pair_sum(l_exact);
-    if (!valid) return;
-    const size_t prow = ((size_t)slot * a.Hkv + g) * ((size_t)a.n_rows * a.G) + (size_t)t * a.G + hh;
-    float* po = a.part_o + prow * D;
+    asm volatile("" : "+v"(lane));
+    __syncthreads();
+    constexpr int OROW = 2 * D + 16;                     // bytes of a row in LDS
+    static_assert(kBaRows * OROW <= (int)sizeof(tiles), "the rows fit the tiles");
+    char* orow = (char*)tiles + (w * 32) * OROW;
+    if (live) {
+        float top = 0.f;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            *(f32x4*)(po + db * 32 + 8 * j + 4 * hf) =
-                f32x4{o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]};
-    if (hf == 0) a.part_s[prow] = float4{m_run, l_tot, l_ex, 0.f};
+            for (int v = 0; v < 16; ++v) {
+                const float x = fabsf(o[db][v]);
+                top = x <= 3.4028235e38f ? fmaxf(top, x) : top;
+            }
+        top = ba_pair_max(top);
+        const float inv = top > 0.f ? 1.0f / top : 1.f;
+        typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *(f16x4*)(orow + (lane & 31) * OROW + 2 * (db * 32 + 8 * j + 4 * (lane >> 5))) =
+                    f16x4{(_Float16)(o[db][4 * j] * inv), (_Float16)(o[db][4 * j + 1] * inv),
+                          (_Float16)(o[db][4 * j + 2] * inv), (_Float16)(o[db][4 * j + 3] * inv)};
+        if (lane < min(n_val, 32)) a.part_s[part + lane] = float4{m_run, l_tot, l_ex, top > 0.f ? top : 1.f};
+        __builtin_amdgcn_wave_barrier();
+        _Float16* dst = a.part_o + part * D + lane * 8;
+#pragma unroll
+        for (int i = 0; i < 32 / RPI; ++i) {
+            const int row = i * RPI + lane / CH;
+            const u32x4 v = *(const u32x4*)(orow + row * OROW + (lane % CH) * 16);
+            if (row < n_val) *(u32x4*)(dst + i * 512) = v;
+        }
+    }
+    if (!ctx || LIST || x >= x_end) return;
+    __syncthreads();                                     // (the next item fills the tiles)
+  }
 }
 
-// D/4 lanes per (token, head): the context slots in order, then the suffix slots that hold
-// one of the row's keys.
-template <int D>
-__global__ __launch_bounds__(256) void batch_merge(const float* __restrict__ part_o,
-                                                   const float4* __restrict__ part_s, int n_ctx,
-                                                   int kss, const int32_t* __restrict__ counts,
-                                                   const int32_t* __restrict__ row_pos, int T, int H,
-                                                   int Hkv, int G, int n_rows,
-                                                   uint16_t* __restrict__ out,
+// D/8 lanes per (token, head): the context partials in order, then the suffix splits that hold
+// one of the row's keys.  A lane takes one partial's statistics; the outputs are then loaded
+// eight at a time with the weights handed round, so a row waits for memory three times.
+template <int D, bool LIST>
+__global__ __launch_bounds__(256) void batch_merge(BaArgs a, uint16_t* __restrict__ out,
                                                    float* __restrict__ lse) {
-    constexpr int LPR = D / 4;
-    const int lane = threadIdx.x % LPR;
+    constexpr int LPR = D / 8;
+    const int lane = threadIdx.x % LPR, base = (threadIdx.x & 63) / LPR * LPR;
     const long th = (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-    const int t = (int)(th / H), h = (int)(th - (long)t * H);
-    if (t >= min(counts[0], n_rows)) return;
-    const int g = h / G;
-    const int n = n_ctx + (row_pos[t] - T) / kss + 1;
-    const size_t stride = (size_t)Hkv * n_rows * G;           // between slots
-    const size_t row = (size_t)g * n_rows * G + (size_t)t * G + (h - g * G);
+    const int t0 = (int)(th / a.H);
+    const BatchSplit sp = load_split(a.counts);
+    // (surplus lanes of a wave follow a real row, so that the exchanges below stay whole)
+    const bool real = t0 < sp.rows;
+    if (!__any(real)) return;                            // (so a step without rows ends here)
+    const int t = real ? t0 : 0, h = real ? (int)(th - (long)t0 * a.H) : 0;
+    const int g = h / a.G, rho = t * a.G + (h - g * a.G);
+    const size_t R = (size_t)sp.rows * a.G;
+    const int n_suf = (a.row_pos[t] - a.T) / sp.suf_kps + 1;
+    int n_ctx;
+    size_t first, step;                                  // context partial s: first + s * step
+    if constexpr (LIST) {
+        int kps;
+        list_split(a, sp.rows, n_ctx, kps);
+        first = (size_t)g * R + rho;
+        step = (size_t)a.Hkv * R;
+    } else {
+        const int chunk = rho / kBaRows, item = g * sp.chunks + chunk;
+        const int64_t x0 = (int64_t)item * sp.len;
+        const int w0 = (int)(x0 / sp.quota);
+        n_ctx = (int)((x0 + sp.tiles - 1) / sp.quota) - w0 + 1;
+        first = (size_t)(w0 + item) * kBaRows + (rho - chunk * kBaRows);
+        step = kBaRows;
+    }
+    const size_t suf = a.suf_part + (size_t)g * R + rho, suf_step = (size_t)a.Hkv * R;
+    const int n = n_ctx + n_suf;
+    auto at = [&](int s) { return s < n_ctx ? first + s * step : suf + (s - n_ctx) * suf_step; };
     float M = -INFINITY;
-    for (int s = lane; s < n; s += LPR) M = fmaxf(M, part_s[s * stride + row].x);
+    float4 st0 = {-INFINITY, 0.f, 0.f, 0.f};
+    for (int s = lane; s < n; s += LPR) {
+        const float4 st = a.part_s[at(s)];
+        if (s == lane) st0 = st;
+        M = fmaxf(M, st.x);
+    }
 #pragma unroll
     for (int o = LPR / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float z = 0.f, ze = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < n; ++s) {
-        const float4 st = part_s[s * stride + row];
-        if (st.x == -INFINITY) continue;                      // (its output is not written)
-        const f32x4 v = *(const f32x4*)(part_o + (s * stride + row) * D + lane * 4);
-        const float wt = fast_exp2(st.x - M);
-        z = fmaf(wt, st.y, z);
-        ze = fmaf(wt, st.z, ze);
-        acc += wt * v;
+    float acc[8], z = 0.f, ze = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    for (int c0 = 0; __any(c0 < n); c0 += LPR) {
+        const int s = c0 + lane;
+        float wt = 0.f;
+        if (s < n) {
+            const float4 st = c0 ? a.part_s[at(s)] : st0;
+            if (st.x != -INFINITY) {
+                const float e = fast_exp2(st.x - M);
+                z = fmaf(e, st.y, z);
+                ze = fmaf(e, st.z, ze);
+                wt = e * st.w;
+            }
+        }
+        typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+        for (int j0 = 0; j0 < LPR && __any(c0 + j0 < n); j0 += 8) {
+            f16x8 v[8];
+            float wj[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                wj[j] = __shfl(wt, base + j0 + j, 64);
+                v[j] = *(const f16x8*)(a.part_o + at(min(c0 + j0 + j, n - 1)) * D + lane * 8);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)              // (weight 0: the output may not be written)
+                    acc[e] = wj[j] != 0.f ? fmaf(wj[j], (float)v[j][e], acc[e]) : acc[e];
+        }
     }
+#pragma unroll
+    for (int o = LPR / 2; o > 0; o >>= 1) {
+        z += __shfl_xor(z, o, 64);
+        ze += __shfl_xor(ze, o, 64);
+    }
+    if (!real) return;
     const float inv = M == -INFINITY ? 0.f : 1.0f / z;
-    uint16_t* dst = out + (size_t)th * D + lane * 4;
-    u32x2 r;
-    r[0] = (uint32_t)f32_to_bf16_bits(acc[0] * inv) | ((uint32_t)f32_to_bf16_bits(acc[1] * inv) << 16);
-    r[1] = (uint32_t)f32_to_bf16_bits(acc[2] * inv) | ((uint32_t)f32_to_bf16_bits(acc[3] * inv) << 16);
-    *(u32x2*)dst = r;
+    u32x4 r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        r[e] = (uint32_t)f32_to_bf16_bits(acc[2 * e] * inv) |
+               ((uint32_t)f32_to_bf16_bits(acc[2 * e + 1] * inv) << 16);
+    *(u32x4*)(out + (size_t)th * D + lane * 8) = r;
     if (lse && lane == 0) lse[th] = M == -INFINITY ? -INFINITY : (M + __log2f(ze)) * kLn2;
 }
 
@@ -504,31 +638,22 @@ __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a
 
 }  // namespace
 
-BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_batch& b, int block,
-                                     int n_sel) {
+// Workgroups of the launch and partial rows of each part: a step of fewer rows than the batch
+// has room for is split further, up to kBaWgs workgroups of kBaRows rows.
+BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_batch& b, int n_sel) {
     BatchAttnWorkspace w = {};
-    if (p.dtype != RELAXKV_DTYPE_BF16) return w;
-    const int G = p.H / p.H_kv;
-    const bool list = n_sel > 0;
-    // Keys per split so that about kBaWgs workgroups are launched, whole tiles, not too few.
-    auto split = [](long keys, long items, int& kps, int& n) {
-        const long want = items >= kBaWgs ? 1 : kBaWgs / items;
-        long k = (keys + want - 1) / want;
-        k = (k + kBaKeys - 1) / kBaKeys * kBaKeys;
-        kps = (int)(k < kBaMinSplit ? kBaMinSplit : k);
-        n = (int)((keys + kps - 1) / kps);
-    };
-    const long rows = (long)b.n_rows * G;
-    w.n_chunks = list ? (G + kBatchRowsBf16 - 1) / kBatchRowsBf16
-                      : (int)((rows + kBatchRowsBf16 - 1) / kBatchRowsBf16);
-    const long ctx_items = (list ? (long)b.n_rows : 1) * p.H_kv * w.n_chunks;
-    const long ctx_keys = list ? (long)n_sel * block : p.T_c;
-    split(ctx_keys, ctx_items > 0 ? ctx_items : 1, w.kps, w.n_ctx);
+    if (p.dtype != RELAXKV_DTYPE_BF16 || b.n_rows == 0) return w;
+    const long G = p.H / p.H_kv, rows = (long)b.n_rows * p.H;
+    const long least = (long)kBaWgs * kBaRows;
+    const long item_cap = (b.n_rows * G + kBaRows - 1) / kBaRows * p.H_kv;
+    const long list_items = (long)b.n_rows * p.H_kv * ((G + kBaRows - 1) / kBaRows);
     const long suf_items = (long)b.tile_cap * p.H_kv;
-    split(b.max_suffix, suf_items > 0 ? suf_items : 1, w.kss, w.n_suf);
-    const size_t slots = (size_t)(w.n_ctx + w.n_suf) * p.H_kv * (size_t)rows;
-    w.part_s_off = (slots * p.d * 4 + 255) / 256 * 256;
-    w.total = w.part_s_off + (slots * 16 + 255) / 256 * 256;
+    w.ctx_wgs = n_sel == 0 ? kBaWgs : (int)(list_items > kBaWgs ? list_items : kBaWgs);
+    w.suf_wgs = (int)(suf_items > kBaWgs ? suf_items : kBaWgs);
+    w.suf_part = n_sel == 0 ? (kBaWgs + item_cap) * kBaRows : rows > least ? rows : least;
+    const size_t parts = w.suf_part + (rows > least ? rows : least);
+    w.part_s_off = (parts * p.d * 2 + 255) / 256 * 256;
+    w.total = w.part_s_off + (parts * 16 + 255) / 256 * 256;
     return w;
 }
 
@@ -589,7 +714,7 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
         }
         return hipGetLastError();
     }
-    const BatchAttnWorkspace w = batch_attn_layout(p, b, block, n_sel);
+    const BatchAttnWorkspace w = batch_attn_layout(p, b, n_sel);
     BaArgs a;
     a.q = (const uint16_t*)q;
     a.kc = (const uint16_t*)k_cache + layer_off;
@@ -602,10 +727,12 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
     a.s_sh = ss.head;
     a.s_st = ss.token;
     a.counts = b.counts;
+    a.row_pos = b.row_pos;
     a.tiles = (const BatchTile*)b.tiles;
     a.lists = blocks;
-    a.part_o = (float*)ws;
+    a.part_o = (_Float16*)ws;
     a.part_s = (float4*)(ws + w.part_s_off);
+    a.suf_part = w.suf_part;
     a.T = p.T_c;
     a.H = p.H;
     a.Hkv = p.H_kv;
@@ -615,27 +742,26 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
     a.bshift = bshift;
     a.nb = nb;
     a.tail = tail;
-    a.n_ctx = w.n_ctx;
-    a.kps = w.kps;
-    a.n_suf = w.n_suf;
-    a.kss = w.kss;
-    a.n_chunks = w.n_chunks;
+    a.ctx_wgs = w.ctx_wgs;
+    a.list_items = p.H_kv * ((G + kBaRows - 1) / kBaRows);
+    a.list_tiles = (int)(((long)n_sel * block + kBaKeys - 1) / kBaKeys);
     a.sl2 = scale * kLog2e;
-    const int pairs = w.n_ctx * p.H_kv;
-    a.ctx_items = list ? b.n_rows * p.H_kv * w.n_chunks * w.n_ctx
-                       : (pairs + kBaXcds - 1) / kBaXcds * kBaXcds * w.n_chunks;
-    const unsigned items = (unsigned)a.ctx_items + (unsigned)(b.tile_cap * p.H_kv * w.n_suf);
-    const unsigned merges = (unsigned)(((long)b.n_rows * p.H * (p.d / 4) + 255) / 256);
-    auto go = [&](auto d_t) {
+    const unsigned merges = (unsigned)(((long)b.n_rows * p.H * (p.d / 8) + 255) / 256);
+    auto go = [&](auto d_t, auto list_t) {
         constexpr int D = decltype(d_t)::value;
-        if (list) hipLaunchKernelGGL((battn_bf16<D, true>), dim3(items), dim3(kBaWaves * 64), 0, st, a);
-        else hipLaunchKernelGGL((battn_bf16<D, false>), dim3(items), dim3(kBaWaves * 64), 0, st, a);
-        hipLaunchKernelGGL((batch_merge<D>), dim3(merges), dim3(256), 0, st, (const float*)a.part_o,
-                           (const float4*)a.part_s, a.n_ctx, a.kss, b.counts, b.row_pos, p.T_c, p.H,
-                           p.H_kv, G, b.n_rows, (uint16_t*)out, lse_out);
+        constexpr bool LIST = decltype(list_t)::value;
+        hipLaunchKernelGGL((battn_bf16<D, LIST>), dim3(w.ctx_wgs + w.suf_wgs), dim3(kBaWaves * 64),
+                           LIST ? n_sel * sizeof(int) : 0, st, a);
+        hipLaunchKernelGGL((batch_merge<D, LIST>), dim3(merges), dim3(256), 0, st, a, (uint16_t*)out,
+                           lse_out);
     };
-    if (p.d == 128) go(Int<128>{});
-    else go(Int<64>{});
+    if (p.d == 128) {
+        if (list) go(Int<128>{}, Int<1>{});
+        else go(Int<128>{}, Int<0>{});
+    } else {
+        if (list) go(Int<64>{}, Int<1>{});
+        else go(Int<64>{}, Int<0>{});
+    }
     return hipGetLastError();
 }
 

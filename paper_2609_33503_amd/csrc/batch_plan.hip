@@ -27,6 +27,15 @@ __device__ __forceinline__ long block_sum(long v, long* scratch) {
     return scratch[0] + scratch[1] + scratch[2] + scratch[3];
 }
 
+__device__ __forceinline__ int block_max(int v, long* scratch) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return (int)max(max(scratch[0], scratch[1]), max(scratch[2], scratch[3]));
+}
+
 // The last entry of the ascending off[0 .. kPlanSeqs] that is <= x (x < off[kPlanSeqs]).
 __device__ __forceinline__ int owner(const int* off, int x) {
     int lo = 0;
@@ -38,7 +47,7 @@ __device__ __forceinline__ int owner(const int* off, int x) {
 
 __global__ __launch_bounds__(kPlanThreads) void batch_plan_rows(
     const int32_t* __restrict__ past_len, const int32_t* __restrict__ new_len, int n_seq,
-    int n_rows, int max_suffix, int T, int G, int tile_rows, int32_t* __restrict__ row_off,
+    int n_rows, int max_suffix, int T, int G, int Hkv, int tile_rows, int32_t* __restrict__ row_off,
     int32_t* __restrict__ row_seq, int32_t* __restrict__ row_pos, BatchTile* __restrict__ tiles,
     int32_t* __restrict__ counts) {
     __shared__ long sums[4];
@@ -54,12 +63,14 @@ __global__ __launch_bounds__(kPlanThreads) void batch_plan_rows(
     };
     auto tiles_of = [&](int n) { return (n * G + tile_rows - 1) / tile_rows; };
     long total = 0, before = 0, tbefore = 0, ttotal = 0, bad = 0;
+    int longest = 0;
     for (int b = tid; b < n_seq; b += kPlanThreads) {
         int n, p;
         if (!lengths(b, n, p)) bad = 1;
         const int t = tiles_of(n);
         total += n;
         ttotal += t;
+        if (n) longest = max(longest, p + n);
         if (b < first) {
             before += n;
             tbefore += t;
@@ -70,7 +81,8 @@ __global__ __launch_bounds__(kPlanThreads) void batch_plan_rows(
     before = block_sum(before, sums);
     tbefore = block_sum(tbefore, sums);
     ttotal = block_sum(ttotal, sums);
-    if (bad) total = before = tbefore = ttotal = 0;
+    longest = block_max(longest, sums);
+    if (bad) total = before = tbefore = ttotal = longest = 0;
     if (tid < kPlanSeqs) {                       // wave 0: one request per lane
         const int b = first + tid;
         int n = 0, p = 0;
@@ -86,8 +98,9 @@ __global__ __launch_bounds__(kPlanThreads) void batch_plan_rows(
             row_off[n_seq] = (int)total;
             counts[0] = (int)total;
             counts[1] = (int)ttotal;
-            counts[2] = 0;
+            counts[2] = longest;
             counts[3] = bad ? RELAXKV_BATCH_ERR_LENGTHS : 0;
+            *(BatchSplit*)(counts + kBatchSplitAt) = batch_split((int)total, (int)ttotal, longest, T, G, Hkv);
         }
     }
     __syncthreads();
@@ -119,7 +132,7 @@ hipError_t launch_batch_plan(const relaxkv_problem& p, const relaxkv_batch& b,
                              const int32_t* past_len, const int32_t* new_len, hipStream_t st) {
     hipLaunchKernelGGL(batch_plan_rows, dim3((b.n_seq + kPlanSeqs - 1) / kPlanSeqs),
                        dim3(kPlanThreads), 0, st, past_len, new_len, b.n_seq, b.n_rows,
-                       b.max_suffix, p.T_c, p.H / p.H_kv, batch_tile_rows(p), b.row_off, b.row_seq,
+                       b.max_suffix, p.T_c, p.H / p.H_kv, p.H_kv, batch_tile_rows(p), b.row_off, b.row_seq,
                        b.row_pos, (BatchTile*)b.tiles, b.counts);
     return hipGetLastError();
 }

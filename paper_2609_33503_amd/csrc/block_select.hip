@@ -13,8 +13,7 @@
 // per row and KV head, against 4 G d per key of the attention that follows.
 //
 // block_means is memory bound (reads every key once); the scores' products are few, and the
-// top-k of up to 4096 blocks runs in the registers of one wave per row, by binary search over
-// the key's bits with no barrier.
+// top-k of up to 4096 blocks searches the bits of the k-th key over keys in registers.
 
 #include <algorithm>
 
@@ -111,17 +110,27 @@ __global__ __launch_bounds__(256) void block_scores(const T* __restrict__ q,
     const T* m = means + ((size_t)g * nb + min(b, nb - 1)) * D;
     float mf[8];
     load8<T>(m + part * 8, mf);
-    for (int x = tid; x < NT * D; x += 256) {
-        const int t = x / D, c = x - t * D;
-        double s = 0.0;
+    // The summed group queries: 8 elements of one row per thread, the heads' loads in flight
+    // together.
+    for (int x = tid; x < NT * D / 8; x += 256) {
+        const int t = x / (D / 8), c = (x - t * (D / 8)) * 8;
+        double s[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = 0.0;
         if (t0 + t < rows) {
             const T* p = q + ((size_t)(t0 + t) * H + g * G) * D + c;
-            for (int h = 0; h < G; ++h) {
-                if constexpr (sizeof(T) == 2) s += (double)bf16_bits_to_f32(p[h * D]);
-                else s += (double)p[h * D];
+            for (int h0 = 0; h0 < G; h0 += 4) {
+                float f[4][8];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) load8<T>(p + min(h0 + h, G - 1) * D, f[h]);
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[e] += h0 + h < G ? (double)f[h][e] : 0.0;
             }
         }
-        qs[t][c] = s;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qs[t][c + e] = s[e];
     }
     __syncthreads();
     double acc[NT];
@@ -158,46 +167,104 @@ __device__ __forceinline__ uint32_t score_key(float f) {
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// One wave per (row, KV head), block e * 64 + lane in register e.  The k-th largest key is
-// the largest t with at least k keys >= t.  Blocks past nb hold key 0; a NaN's key 0
+// Sum over the wave's lanes, as a uniform value.
+__device__ __forceinline__ uint32_t wave_total(uint32_t x) {
+    x += __builtin_amdgcn_update_dpp(0u, x, 0x111, 0xf, 0xf, true);    // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0u, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0u, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0u, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0u, x, 0x142, 0xa, 0xf, true);    // row_bcast:15, 31
+    x += __builtin_amdgcn_update_dpp(0u, x, 0x143, 0xc, 0xf, true);
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
+// One workgroup of W waves per (row, KV head): wave w holds the 8 * 64 blocks from w * 512,
+// block e * 64 + lane of them in register e.  The k-th largest key is the largest t with at
+// least k keys >= t, found two bits at a time: the three counts that decide a step are at
+// most 512 per wave and go through the wave's sum packed in 10 bits each, then through LDS.
+// (2048 blocks, k 32, 64 rows of KV heads: 4.6 us; one wave per row and one bit at a time by
+// ballots, which the scalar unit counts, 42 us.)  Blocks past nb hold key 0; a NaN's key 0
 // lies at a lower block, and k <= nb, so none of them is ever taken.
-template <int E>
-__global__ __launch_bounds__(256) void block_topk_wave(const float* __restrict__ scores, int nb,
-                                                       int k, const int32_t* __restrict__ counts,
-                                                       int n_rows, int Hkv,
-                                                       int32_t* __restrict__ out) {
-    const long unit = blockIdx.x * 4l + (threadIdx.x >> 6);
+template <int W>
+__global__ __launch_bounds__(W * 64) void block_topk_reg(const float* __restrict__ scores, int nb,
+                                                         int k, const int32_t* __restrict__ counts,
+                                                         int n_rows, int Hkv,
+                                                         int32_t* __restrict__ out) {
+    constexpr int E = 8;
+    __shared__ uint32_t part[2][W];
+    const long unit = blockIdx.x;
     const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (unit >= (long)min(counts[0], n_rows) * Hkv) return;
     const float* s = scores + unit * nb;
+    const int i0 = w * (E * 64) + lane;
     uint32_t key[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int i = e * 64 + lane;
-        key[e] = i < nb ? score_key(s[i]) : 0u;
-    }
+    for (int e = 0; e < E; ++e) key[e] = i0 + e * 64 < nb ? score_key(s[i0 + e * 64]) : 0u;
+    // The sum over the workgroup of three counts of at most 512 per wave (c in 10-bit fields).
+    auto total3 = [&](uint32_t c, int turn, int& n1, int& n2, int& n3) {
+        c = wave_total(c);
+        if constexpr (W == 1) {
+            n1 = c & 1023;
+            n2 = c >> 10 & 1023;
+            n3 = c >> 20;
+        } else {
+            if (lane == 0) part[turn & 1][w] = c;
+            __syncthreads();
+            n1 = n2 = n3 = 0;
+#pragma unroll
+            for (int x = 0; x < W; ++x) {
+                const uint32_t p = part[turn & 1][x];
+                n1 += p & 1023;
+                n2 += p >> 10 & 1023;
+                n3 += p >> 20;
+            }
+        }
+    };
     uint32_t t = 0;
 #pragma unroll 1
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t cand = t | (1u << bit);
-        int n = 0;
+    for (int bit = 30; bit >= 0; bit -= 2) {
+        uint32_t c1 = 0, c2 = 0, c3 = 0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) n += __popcll(__ballot(key[e] >= cand));
-        if (n >= k) t = cand;
+        for (int e = 0; e < E; ++e) {
+            c1 += key[e] >= (t | 1u << bit);
+            c2 += key[e] >= (t | 2u << bit);
+            c3 += key[e] >= (t | 3u << bit);
+        }
+        int n1, n2, n3;
+        total3(c1 | c2 << 10 | c3 << 20, bit >> 1, n1, n2, n3);
+        t |= (n3 >= k ? 3u : n2 >= k ? 2u : n1 >= k ? 1u : 0u) << bit;
     }
-    int above = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) above += __popcll(__ballot(key[e] > t));
-    const int need = k - above;                      // of the keys equal to t, the first ones
-    int gt0 = 0, eq0 = 0;
+    // Every key above t, and of those equal to it the first `need`; in block order.
+    int gt0 = 0, eq0 = 0, above = 0;
+    uint64_t mg[E], me[E];
+    uint32_t own = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const uint64_t mg = __ballot(key[e] > t), me = __ballot(key[e] == t);
-        const int gt = gt0 + lanes_below(mg), eq = eq0 + lanes_below(me);
-        if (key[e] > t || (key[e] == t && eq < need))
-            out[unit * k + gt + min(eq, need)] = e * 64 + lane;
-        gt0 += __popcll(mg);
-        eq0 += __popcll(me);
+        mg[e] = __ballot(key[e] > t);
+        me[e] = __ballot(key[e] == t);
+        own += (uint32_t)__popcll(mg[e]) | (uint32_t)__popcll(me[e]) << 16;
+    }
+    if constexpr (W == 1) {
+        above = own & 0xffff;
+    } else {
+        if (lane == 0) part[1][w] = own;               // (the last turn above used part[0])
+        __syncthreads();
+#pragma unroll
+        for (int x = 0; x < W; ++x) {
+            const uint32_t p = part[1][x];
+            above += p & 0xffff;
+            gt0 += x < w ? p & 0xffff : 0;
+            eq0 += x < w ? p >> 16 : 0;
+        }
+    }
+    const int need = k - above;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int gt = gt0 + lanes_below(mg[e]), eq = eq0 + lanes_below(me[e]);
+        if (key[e] > t || (key[e] == t && eq < need)) out[unit * k + gt + min(eq, need)] = i0 + e * 64;
+        gt0 += __popcll(mg[e]);
+        eq0 += __popcll(me[e]);
     }
 }
 
@@ -300,14 +367,15 @@ hipError_t launch_block_select(const relaxkv_problem& p, const relaxkv_batch& b,
     }
     const int nb = block_count(p, block);
     const long units = (long)b.n_rows * p.H_kv;
-    auto go = [&](auto kernel, long per_wg) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((units + per_wg - 1) / per_wg)), dim3(256), 0, st,
-                           scores, nb, n_sel, b.counts, b.n_rows, p.H_kv, blocks);
+    auto go = [&](auto kernel, int waves) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3(waves * 64), 0, st, scores, nb, n_sel,
+                           b.counts, b.n_rows, p.H_kv, blocks);
     };
-    if (nb <= 4 * 64) go(block_topk_wave<4>, 4);
-    else if (nb <= 16 * 64) go(block_topk_wave<16>, 4);
-    else if (nb <= 64 * 64) go(block_topk_wave<64>, 4);
-    else go(block_topk_long, 1);
+    if (nb <= 512) go(block_topk_reg<1>, 1);
+    else if (nb <= 1024) go(block_topk_reg<2>, 2);
+    else if (nb <= 2048) go(block_topk_reg<4>, 4);
+    else if (nb <= 4096) go(block_topk_reg<8>, 8);
+    else go(block_topk_long, 4);
     return hipGetLastError();
 }
 

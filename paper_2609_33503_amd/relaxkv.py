@@ -763,7 +763,7 @@ class Batch:
         self.counts = view(s.counts, 4)
 
     def counts_to_host(self, stream=None, check=True):
-        """[rows, row tiles, 0, error word] of the planned step on the host; synchronises the
+        """[rows, row tiles, longest suffix, error word] of the planned step on the host; synchronises the
         stream.  With check=True a set error word raises RelaxKVError."""
         c = (c_int32 * 4)()
         st = load().relaxkv_batch_to_host(self.ref, c, _stream(stream))

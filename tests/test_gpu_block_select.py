@@ -147,7 +147,8 @@ def test_plan(gpu_lib, past, new, n_rows, H, H_kv, dtype):
         got = got.cpu().numpy()
         assert np.array_equal(got[:n], want) and np.all(got[n:] == -1)
     tiles = [(s, off[s], k, past[s], r) for s, k in enumerate(new) for r in range(0, k * G, tile)]
-    assert b.counts_to_host() == [n, len(tiles), 0, 0]
+    longest = max([p + k for p, k in zip(past, new) if k], default=0)
+    assert b.counts_to_host() == [n, len(tiles), longest, 0]
     at = b.s.tiles - b.buf.data_ptr()
     rec = b.buf[at:at + 32 * len(tiles)].view(torch.int32).view(-1, 8).cpu().numpy()
     assert np.array_equal(rec[:, :5], np.array(tiles, dtype=np.int64).reshape(-1, 5))
