@@ -285,7 +285,9 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = f32x16{};
     // The row's reference maximum, what the logits are compared with, and subtracted from them.
-    float m_run = -INFINITY, thr = -INFINITY, m_ref = 0.f, l_run = 0.f, l_exact = 0.f;
+    float m_run = -INFINITY, thr = -INFINITY, m_ref = 0.f;
+    float l0 = 0.f, l1 = 0.f, e0 = 0.f, e1 = 0.f;        // sums of rounded and exact probabilities
+    const float inv_sl2 = 1.0f / a.sl2;
 
     // Loader: load jj = w + NW i fills tile rows jj RPI ..; lane l writes (row l / CH, chunk
     // l % CH) and fetches the chunk that belongs there.  The swizzle of a lane's rows is the
@@ -376,12 +378,15 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
             mk = fmaxf(fmaxf(mk, s[v]), s[v + 1]);
             mk2 = fmaxf(fmaxf(mk2, s[v + 2]), s[v + 3]);
         }
-        const float mx = ba_pair_max(fmaxf(mk, mk2)) * a.sl2;
-        if (__any(mx > thr)) {
+        const float top = ba_pair_max(fmaxf(mk, mk2));
+        if (__any(top > thr)) {
+            const float mx = top * a.sl2;
             const float m_new = mx > m_run + kBaSlack ? mx : m_run;
             const float alpha = m_new == m_run ? 1.f : fast_exp2(m_run - m_new);
-            l_run *= alpha;
-            l_exact *= alpha;
+            l0 *= alpha;
+            l1 *= alpha;
+            e0 *= alpha;
+            e1 *= alpha;
 #pragma unroll
             for (int db = 0; db < DB; ++db) o[db] *= alpha;
             m_run = m_new;
@@ -391,36 +396,32 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
             // the product rounded too and its logits moved to a maximum of 0.
             const bool none = m_run == -INFINITY, huge = !none && fabsf(m_run) > kBaHuge;
             m_ref = none || huge ? 0.f : m_run;          // (no visible key so far: exact zeros)
-            thr = huge ? -INFINITY : m_run + kBaSlack;
+            thr = huge ? -INFINITY : (m_run + kBaSlack) * inv_sl2;
             if (__any(huge)) {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     float x = s[v] * a.sl2;
                     asm volatile("" : "+v"(x));          // (not a multiply-add)
-                    s[v] = huge ? (x - m_run) * (1.0f / a.sl2) : s[v];
+                    s[v] = huge ? (x - m_run) * inv_sl2 : s[v];
                 }
             }
         }
         bf16x8 pb[2];
-        float e0 = 0.f, e1 = 0.f;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             const float p = fast_exp2(fmaf(s[v], a.sl2, -m_ref));
             (v & 1 ? e1 : e0) += p;
             pb[v >> 3][v & 7] = (__bf16)p;
         }
-        l_exact += e0 + e1;
         const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
-        float ls0 = 0.f, ls1 = 0.f;
 #pragma unroll
         for (int k2 = 0; k2 < 2; ++k2) {
             const bf16x8 q8 = pb[k2];
-            ls0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 0, 1), one2, ls0, false);
-            ls1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 2, 3), one2, ls1, false);
-            ls0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 4, 5), one2, ls0, false);
-            ls1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 6, 7), one2, ls1, false);
+            l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 0, 1), one2, l0, false);
+            l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 2, 3), one2, l1, false);
+            l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 4, 5), one2, l0, false);
+            l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 6, 7), one2, l1, false);
         }
-        l_run += ls0 + ls1;
         // O^T += V^T P^T
 #pragma unroll
         for (int y = 0; y < 2 * DB; ++y) {
@@ -444,7 +445,7 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
 
     // The partial rows: scaled by the largest finite element, transposed through LDS (the
     // tiles are done with) and written as whole rows.
-    const float l_tot = ba_pair_sum(l_run), l_ex = ba_pair_sum(l_exact);
+    const float l_tot = ba_pair_sum(l0 + l1), l_ex = ba_pair_sum(e0 + e1);
     asm volatile("" : "+v"(lane));
     __syncthreads();
     constexpr int OROW = 2 * D + 16;                     // bytes of a row in LDS
@@ -484,20 +485,21 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
   }
 }
 
-// D/8 lanes per (token, head): the context partials in order, then the suffix splits that hold
-// one of the row's keys.  A lane takes one partial's statistics; the outputs are then loaded
-// eight at a time with the weights handed round, so a row waits for memory three times.
-template <int D, bool LIST>
-__global__ __launch_bounds__(256) void batch_merge(BaArgs a, uint16_t* __restrict__ out,
-                                                   float* __restrict__ lse) {
-    constexpr int LPR = D / 8;
-    const int lane = threadIdx.x % LPR, base = (threadIdx.x & 63) / LPR * LPR;
-    const long th = (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+// LN lanes per (token, head): its partials are the context's in order, then the suffix splits
+// that hold one of the row's keys.  Lane i takes the statistics of partial i (then i + LN, ..);
+// the outputs are loaded by groups of D/8 lanes, partial by partial in turn, four each at a
+// time with the weights handed round, so a row waits for memory about three times.
+template <int D, bool LIST, int LN>
+__device__ __forceinline__ void merge_row(const BaArgs& a, const BatchSplit& sp, long th,
+                                          uint16_t* __restrict__ out, float* __restrict__ lse) {
+    constexpr int LPR = D / 8, NG = LN / LPR, U = 4;
+    typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+    const int wl = threadIdx.x & 63, base = wl / LN * LN, lane = wl - base;
+    const int grp = lane / LPR, col = lane % LPR;
     const int t0 = (int)(th / a.H);
-    const BatchSplit sp = load_split(a.counts);
     // (surplus lanes of a wave follow a real row, so that the exchanges below stay whole)
     const bool real = t0 < sp.rows;
-    if (!__any(real)) return;                            // (so a step without rows ends here)
+    if (!__any(real)) return;
     const int t = real ? t0 : 0, h = real ? (int)(th - (long)t0 * a.H) : 0;
     const int g = h / a.G, rho = t * a.G + (h - g * a.G);
     const size_t R = (size_t)sp.rows * a.G;
@@ -520,60 +522,75 @@ __global__ __launch_bounds__(256) void batch_merge(BaArgs a, uint16_t* __restric
     const size_t suf = a.suf_part + (size_t)g * R + rho, suf_step = (size_t)a.Hkv * R;
     const int n = n_ctx + n_suf;
     auto at = [&](int s) { return s < n_ctx ? first + s * step : suf + (s - n_ctx) * suf_step; };
-    float M = -INFINITY;
-    float4 st0 = {-INFINITY, 0.f, 0.f, 0.f};
-    for (int s = lane; s < n; s += LPR) {
-        const float4 st = a.part_s[at(s)];
-        if (s == lane) st0 = st;
-        M = fmaxf(M, st.x);
-    }
+    const float4 none = {-INFINITY, 0.f, 0.f, 0.f};
+    const float4 st0 = lane < n ? a.part_s[at(lane)] : none;
+    float M = st0.x;
+    for (int s = lane + LN; s < n; s += LN) M = fmaxf(M, a.part_s[at(s)].x);
 #pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+    for (int o = LN / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
     float acc[8], z = 0.f, ze = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-    for (int c0 = 0; __any(c0 < n); c0 += LPR) {
-        const int s = c0 + lane;
-        float wt = 0.f;
-        if (s < n) {
-            const float4 st = c0 ? a.part_s[at(s)] : st0;
-            if (st.x != -INFINITY) {
-                const float e = fast_exp2(st.x - M);
-                z = fmaf(e, st.y, z);
-                ze = fmaf(e, st.z, ze);
-                wt = e * st.w;
-            }
-        }
-        typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-        for (int j0 = 0; j0 < LPR && __any(c0 + j0 < n); j0 += 8) {
-            f16x8 v[8];
-            float wj[8];
+    for (int c0 = 0; __any(c0 < n); c0 += LN) {
+        const float4 st = c0 == 0 ? st0 : c0 + lane < n ? a.part_s[at(c0 + lane)] : none;
+        const float e = st.x == -INFINITY ? 0.f : fast_exp2(st.x - M);
+        z = fmaf(e, st.y, z);
+        ze = fmaf(e, st.z, ze);
+        const float wt = e * st.w;                       // (0 past the last partial)
+        for (int j0 = 0; j0 < LN && __any(c0 + j0 < n); j0 += NG * U) {
+            f16x8 v[U];
+            float wj[U];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                wj[j] = __shfl(wt, base + j0 + j, 64);
-                v[j] = *(const f16x8*)(a.part_o + at(min(c0 + j0 + j, n - 1)) * D + lane * 8);
+            for (int u = 0; u < U; ++u) {
+                const int j = j0 + u * NG + grp;
+                wj[u] = __shfl(wt, base + (j & (LN - 1)), 64);
+                v[u] = *(const f16x8*)(a.part_o + at(min(c0 + j, n - 1)) * D + col * 8);
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int e = 0; e < 8; ++e)              // (weight 0: the output may not be written)
-                    acc[e] = wj[j] != 0.f ? fmaf(wj[j], (float)v[j][e], acc[e]) : acc[e];
+                for (int i = 0; i < 8; ++i)              // (weight 0: the output may not be written)
+                    acc[i] = wj[u] != 0.f ? fmaf(wj[u], (float)v[u][i], acc[i]) : acc[i];
         }
     }
 #pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) {
+    for (int o = LN / 2; o > 0; o >>= 1) {
         z += __shfl_xor(z, o, 64);
         ze += __shfl_xor(ze, o, 64);
     }
+#pragma unroll
+    for (int o = LPR; o < LN; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] += __shfl_xor(acc[i], o, 64);
     if (!real) return;
     const float inv = M == -INFINITY ? 0.f : 1.0f / z;
-    u32x4 r;
+    if (grp == 0) {
+        u32x4 r;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        r[e] = (uint32_t)f32_to_bf16_bits(acc[2 * e] * inv) |
-               ((uint32_t)f32_to_bf16_bits(acc[2 * e + 1] * inv) << 16);
-    *(u32x4*)(out + (size_t)th * D + lane * 8) = r;
+        for (int i = 0; i < 4; ++i)
+            r[i] = (uint32_t)f32_to_bf16_bits(acc[2 * i] * inv) |
+                   ((uint32_t)f32_to_bf16_bits(acc[2 * i + 1] * inv) << 16);
+        *(u32x4*)(out + (size_t)th * D + col * 8) = r;
+    }
     if (lse && lane == 0) lse[th] = M == -INFINITY ? -INFINITY : (M + __log2f(ze)) * kLn2;
+}
+
+// A row takes a wave where that makes one round of waves, and where it has many partials (9
+// partials of 256 rows: 4.4 us, 5.7 with D/8 lanes per row; 33 of 2440: 9.0, 10.2); else D/8
+// lanes (5 partials of 24352 rows: 12.3 us, 20.7 with a wave).
+constexpr int kBaManyPartials = 16, kBaWaveRows = 8192;
+template <int D, bool LIST>
+__global__ __launch_bounds__(256) void batch_merge(BaArgs a, uint16_t* __restrict__ out,
+                                                   float* __restrict__ lse) {
+    constexpr int LPR = D / 8;
+    const BatchSplit sp = load_split(a.counts);
+    int n_ctx, kps;
+    if constexpr (LIST) list_split(a, sp.rows, n_ctx, kps);
+    else n_ctx = sp.tiles / sp.quota + 1;
+    if (n_ctx + sp.suf_n > kBaManyPartials || sp.rows * a.H <= kBaWaveRows)
+        merge_row<D, LIST, 64>(a, sp, blockIdx.x * 4l + (threadIdx.x >> 6), out, lse);
+    else
+        merge_row<D, LIST, LPR>(a, sp, (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR, out, lse);
 }
 
 // float32: rows of one request per workgroup; key c is context key c (or listed key c) below
@@ -746,7 +763,7 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
     a.list_items = p.H_kv * ((G + kBaRows - 1) / kBaRows);
     a.list_tiles = (int)(((long)n_sel * block + kBaKeys - 1) / kBaKeys);
     a.sl2 = scale * kLog2e;
-    const unsigned merges = (unsigned)(((long)b.n_rows * p.H * (p.d / 8) + 255) / 256);
+    const unsigned merges = (unsigned)(((long)b.n_rows * p.H + 3) / 4);
     auto go = [&](auto d_t, auto list_t) {
         constexpr int D = decltype(d_t)::value;
         constexpr bool LIST = decltype(list_t)::value;

@@ -329,6 +329,7 @@ class Request:
         self._cache_shape, self._cache_stride = (L, H_kv, T_c, d), k_cache.stride()
         self._scores_shape = (L, T_c)
         self._q_shape, self._kq_shape, self._lse_shape = (Qn, H, d), (Qn, H_kv, d), (Qn, H)
+        self._batch_key = (T_c, H, H_kv, d, self.dtype, self._index)
 
     @property
     def p(self):
@@ -540,26 +541,32 @@ class Request:
         return _stream(stream)
 
     def _batch(self, batch):
-        if type(batch) is not Batch or batch.key != (self.T_c, self.H, self.H_kv, self.d, self.dtype,
-                                                     self._index):
+        if type(batch) is not Batch or batch.key != self._batch_key:
             raise ValueError("batch must come from alloc_batch() of a request of this shape")
 
     def _suffix(self, batch, k, v):
         """The suffix caches' descriptor (the library checks the strides)."""
-        shape = (batch.n_seq, self.H_kv, batch.max_suffix, self.d)
+        shape = batch.suffix_shape
         for t, name in ((k, "k_suffix"), (v, "v_suffix")):
-            if not (type(t) is _Tensor and t.dtype is self.dtype and t.is_cuda
-                    and t.get_device() == self._index and t.shape == shape and t.stride(3) == 1):
+            if not (type(t) is _Tensor and t.dtype is self.dtype and t.shape == shape and t.is_cuda
+                    and t.get_device() == self._index and t.stride(3) == 1):
                 _need_cache(t, name, self.dtype, shape, self.device)
-        if k.stride() != v.stride() and _cache_strides(k) != _cache_strides(v):
-            raise ValueError("k_suffix and v_suffix must have the same strides")
-        return CSuffix(k.data_ptr(), v.data_ptr(), *_cache_strides(k))
+        st = k.stride()
+        if st != v.stride() or batch.flat:                # (a dimension of size 1: any stride)
+            st = _cache_strides(k)
+            if st != _cache_strides(v):
+                raise ValueError("k_suffix and v_suffix must have the same strides")
+        return CSuffix(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2])
 
     def _projected(self, t, name, heads, n):
-        """A [n][heads][d] tensor whose rows are contiguous (any row stride); its row stride
-        for the library."""
+        """The row stride of a [n][heads][d] tensor whose rows are contiguous."""
         if t is None:
             return 0
+        if type(t) is _Tensor and t.dtype is self.dtype and t.is_cuda \
+                and t.get_device() == self._index and t.shape == (n, heads, self.d):
+            st = t.stride()
+            if st[2] == 1 and st[1] == self.d and n > 1:
+                return st[0]
         if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != self.dtype:
             raise ValueError(f"{name} must be a {self.dtype} tensor on {self.device}")
         _need_shape(t, name, (n, heads, self.d))
@@ -574,13 +581,11 @@ class Request:
     def _rope(self, rope):
         if type(rope) is not Rope:
             raise ValueError("rope must be a Rope")
-        for t in (rope.inv_freq, rope.q_weight, rope.k_weight):
-            if t is not None and t.device != self.device:
-                raise ValueError(f"rope's tensors must be on {self.device}")
-        for t, name in ((rope.q_weight, "q_weight"), (rope.k_weight, "k_weight")):
-            if t is not None:
-                self._want(t, name, self.dtype, (self.d,))
-        return ctypes.byref(rope.s)
+        for device, dtype, d in rope.tensors:
+            if device != self._index or dtype not in (None, self.dtype) or d not in (None, self.d):
+                raise ValueError(f"rope's tensors must be on {self.device}, its norm weights "
+                                 f"[{self.d}] {self.dtype}")
+        return rope.ref
 
     def plan_batch(self, batch, past_len, new_len, stream=None):
         """past_len and new_len [n_seq] int32 device: tokens of each request's suffix before
@@ -601,10 +606,10 @@ class Request:
         rows = self._rows(q, k, v, n)
         for t, o, name, heads in ((q, q_out, "q_out", self.H), (k, k_out, "k_out", self.H_kv),
                                   (v, v_out, "v_out", self.H_kv)):
-            if (t is None) != (o is None):
-                raise ValueError(f"{name} and its input must both be given, or neither")
             if o is not None:
                 self._want(o, name, self.dtype, (n, heads, self.d))
+            if (t is None) != (o is None):
+                raise ValueError(f"{name} and its input must both be given, or neither")
         _check(self._lib.relaxkv_fresh_rows(self._ref, self._rope(rope), ctypes.byref(rows),
                                             positions.data_ptr(), _ptr(q_out), _ptr(k_out),
                                             _ptr(v_out), self._here(stream)), "relaxkv_fresh_rows")
@@ -737,11 +742,17 @@ class Rope:
                                      or not inv_freq.is_contiguous()):
             raise ValueError("inv_freq must be a contiguous float32 tensor [rot/2]")
         for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-            if t is not None and not isinstance(t, torch.Tensor):
-                raise ValueError(f"{name} must be a tensor or None")
+            if t is not None and not (isinstance(t, torch.Tensor) and t.dim() == 1
+                                      and t.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous tensor [d] or None")
         self.inv_freq, self.q_weight, self.k_weight = inv_freq, q_weight, k_weight
+        # what a request checks: device (-1 for the host), dtype and length of each tensor
+        self.tensors = [(t.get_device(), None if t is inv_freq else t.dtype,
+                         None if t is inv_freq else t.shape[0])
+                        for t in (inv_freq, q_weight, k_weight) if t is not None]
         self.s = CRope(_ptr(inv_freq), _ptr(q_weight), _ptr(k_weight), float(eps),
                        0 if inv_freq is None else 2 * inv_freq.shape[0], 1 if interleaved else 0)
+        self.ref = ctypes.byref(self.s)
 
 
 class Batch:
@@ -751,6 +762,8 @@ class Batch:
         self.buf, self.s, self.ref = buf, s, ctypes.byref(s)
         self.n_seq, self.n_rows, self.max_suffix = s.n_seq, s.n_rows, s.max_suffix
         self.key = (req.T_c, req.H, req.H_kv, req.d, req.dtype, req._index)
+        self.suffix_shape = (s.n_seq, req.H_kv, s.max_suffix, req.d)
+        self.flat = 1 in self.suffix_shape[:3]
         base = buf.data_ptr()
 
         def view(ptr, n):
