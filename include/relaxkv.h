@@ -616,7 +616,7 @@ relaxkv_status relaxkv_batch_rows(const relaxkv_problem* p, const relaxkv_rope* 
                                   const relaxkv_batch* b, const relaxkv_rows* in, void* q_out,
                                   const relaxkv_suffix* suffix, void* stream);
 
-/* Host only.  Device scratch bytes of relaxkv_shared_attn (0 for float32, and for bad
+/* Host only.  Device scratch bytes of relaxkv_shared_attn (0 without rows, and for bad
  * arguments). */
 size_t relaxkv_shared_attn_workspace_bytes(const relaxkv_problem* p, const relaxkv_batch* b);
 
@@ -669,7 +669,8 @@ relaxkv_status relaxkv_block_select(const relaxkv_problem* p, const relaxkv_batc
                                     const void* means, const void* q, int32_t n_sel,
                                     int32_t* blocks, void* ws, size_t ws_bytes, void* stream);
 
-/* Host only.  Device scratch bytes of relaxkv_block_attn (0 for float32 and bad arguments). */
+/* Host only.  Device scratch bytes of relaxkv_block_attn (0 without rows, and for bad
+ * arguments). */
 size_t relaxkv_block_attn_workspace_bytes(const relaxkv_problem* p, const relaxkv_batch* b,
                                           int32_t block, int32_t n_sel);
 

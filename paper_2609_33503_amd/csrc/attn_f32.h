@@ -88,8 +88,9 @@ struct AttnF32Lds {
 // visible key, -1 for none (the row is then the empty sum: O = 0, lse = -inf).
 // A row's result depends on no K or V it does not see, not even on a NaN there.
 // n_keys > every row's limit.  The lane's row is row orow of out [][D] and lse_out
-// (may be null); written only if `valid`.
-template <int D, int R, typename IdOf>
+// (may be null); written only if `valid`.  NACC: accumulators of a logit; its products go to
+// them in turn and they are added at the end, so that fewer roundings follow one another.
+template <int D, int R, int NACC = 1, typename IdOf>
 __device__ __forceinline__ void attn_f32_rows(AttnF32Lds<D, R>& sm, const float* kn,
                                               const float* vn, int64_t fs, const float* kc,
                                               const float* vc, int64_t cs, IdOf id_of, int n_keys,
@@ -148,13 +149,18 @@ __device__ __forceinline__ void attn_f32_rows(AttnF32Lds<D, R>& sm, const float*
         const int bn = b + NW;
         const bool more = bn * R < n_keys;
         const int id_n = more ? id_at(bn) : 0;
-        Acc s = Acc{};
+        Acc sa[NACC];
+#pragma unroll
+        for (int i = 0; i < NACC; ++i) sa[i] = Acc{};
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const f32x4 qj = sm.q[j][lane];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s = M32::mac(kf[j][i], qj[i], s);
+            for (int i = 0; i < 4; ++i) sa[i % NACC] = M32::mac(kf[j][i], qj[i], sa[i % NACC]);
         }
+        Acc s = sa[0];
+        if constexpr (NACC == 4) s = (sa[0] + sa[1]) + (sa[2] + sa[3]);
+        static_assert(NACC == 1 || NACC == 4, "accumulators");
         if (more) load_k(id_n);
         const int ex = lim - b * R;
         float mx = -INFINITY;

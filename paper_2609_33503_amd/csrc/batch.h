@@ -35,6 +35,9 @@ constexpr int kBaKeys = 32;            // keys per tile
 constexpr int kBaWgs = 768;            // workgroups the splits aim for (three per CU)
 constexpr int kBaMinTiles = 8;         // fewest tiles per split
 constexpr int kBaXcds = 8;
+// float32: a split's keys are at least one block for each of the 16 waves, its workgroups one
+// round (one per CU at d 128).
+constexpr int kBaF32Keys = 256, kBaF32Wgs = 256;
 constexpr int kBatchSplitAt = 16;      // first word of the split in relaxkv_batch::counts
 
 // Shared context: item (g, chunk) = g * chunks + chunk holds `tiles` key tiles, worker w takes
@@ -50,13 +53,16 @@ struct BatchSplit {
     int32_t chunks, items, tiles, len, quota, workers;
     int32_t per_item;                  // workers of an item; 0: cut anywhere
     int32_t suf_n, suf_kps;            // suffix splits, keys each
+    int32_t f32_n, f32_kps;            // float32: splits of a row tile's keys, keys each
 };
 
-// Splits n of `tiles` key tiles, `quota` tiles each, so that `items` of them fill the chip.
-__host__ __device__ inline void batch_split_keys(int tiles, int items, int& n, int& quota) {
-    const int want = items >= kBaWgs ? 1 : kBaWgs / (items > 0 ? items : 1);
+// Splits n of `tiles` key tiles, `quota` (at least `least`) tiles each, so that `items` of them
+// are about `wgs` workgroups.
+__host__ __device__ inline void batch_split_keys(int tiles, int items, int wgs, int least, int& n,
+                                                 int& quota) {
+    const int want = items >= wgs ? 1 : wgs / (items > 0 ? items : 1);
     quota = (tiles + want - 1) / want;
-    quota = quota < kBaMinTiles ? kBaMinTiles : quota;
+    quota = quota < least ? least : quota;
     n = tiles > 0 ? (tiles + quota - 1) / quota : 1;
 }
 
@@ -86,8 +92,12 @@ __host__ __device__ inline BatchSplit batch_split(int rows, int row_tiles, int l
         s.workers = (int32_t)((all + s.quota - 1) / s.quota);
     }
     int quota;
-    batch_split_keys((longest + kBaKeys - 1) / kBaKeys, row_tiles * Hkv, s.suf_n, quota);
+    batch_split_keys((longest + kBaKeys - 1) / kBaKeys, row_tiles * Hkv, kBaWgs, kBaMinTiles, s.suf_n,
+                     quota);
     s.suf_kps = quota * kBaKeys;
+    batch_split_keys((T + longest + kBaF32Keys - 1) / kBaF32Keys, row_tiles * Hkv, kBaF32Wgs, 1, s.f32_n,
+                     s.f32_kps);
+    s.f32_kps *= kBaF32Keys;
     return s;
 }
 

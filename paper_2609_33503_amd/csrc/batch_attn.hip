@@ -29,8 +29,9 @@
 // Loads never leave a run's keys (past its end they repeat its last key, masked), so cache
 // rows past the context and suffix tokens past a request's length are never read.
 //
-// float32: the MFMA core of attn_f32.h, 16 rows of one request per workgroup over all of
-// their keys.
+// float32: the MFMA core of attn_f32.h, 16 rows of one request per workgroup over one split of
+// their context and suffix keys; with more than one split they write normalised outputs and
+// log-sum-exps, which batch_merge_f32 adds in split order.
 
 #include <math.h>
 
@@ -86,7 +87,7 @@ __device__ __forceinline__ BatchSplit load_split(const int32_t* counts) {
 // Listed keys of a row: splits, keys of each.
 __device__ __forceinline__ void list_split(const BaArgs& a, int rows, int& n, int& kps) {
     const int tiles = a.list_tiles;
-    batch_split_keys(tiles, rows * a.list_items, n, kps);
+    batch_split_keys(tiles, rows * a.list_items, kBaWgs, kBaMinTiles, n, kps);
     kps *= kBaKeys;
 }
 
@@ -601,9 +602,23 @@ struct BaF32Args {
     const int32_t *counts, *row_seq, *row_pos, *lists;
     const BatchTile* tiles;
     int T, H, Hkv, G, n_rows, n_sel, bshift, nb, tail;
+    int list_tiles, list_items;      // listed: kBaF32Keys of a row at most (and its suffix), items
     float scale;
     float *out, *lse;
+    float *part_o, *part_l;          // [split][rows of the step][H] (D)
 };
+
+// Splits of a row tile's keys.
+template <bool LIST>
+__device__ __forceinline__ void f32_split(const BaF32Args& a, const BatchSplit& sp, int& n, int& kps) {
+    n = sp.f32_n;
+    kps = sp.f32_kps;
+    if constexpr (LIST) {
+        batch_split_keys(a.list_tiles + (a.counts[2] + kBaF32Keys - 1) / kBaF32Keys,
+                         sp.rows * a.list_items, kBaF32Wgs, 1, n, kps);
+        kps *= kBaF32Keys;
+    }
+}
 
 template <int D, bool LIST>
 __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a) {
@@ -611,15 +626,22 @@ __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a
     extern __shared__ __attribute__((aligned(16))) char f32_lds[];
     AttnF32Lds<D, R>& sm = *(AttnF32Lds<D, R>*)f32_lds;
     int* lst = (int*)(f32_lds + sizeof(AttnF32Lds<D, R>));
-    const int g = blockIdx.y, rl = threadIdx.x % R;
-    const int rows = min(a.counts[0], a.n_rows);
+    const int rl = threadIdx.x % R;
+    const BatchSplit sp = load_split(a.counts);
+    int n_split, kps;
+    f32_split<LIST>(a, sp, n_split, kps);
+    int x = blockIdx.x;
+    const int split = x % n_split;
+    x /= n_split;
+    const int g = x % a.Hkv;
+    x /= a.Hkv;
     int t, hh, seq, own, last_own, n_ctx = a.T;
     bool valid;
     if constexpr (LIST) {
         const int chunks = (a.G + R - 1) / R;
-        t = blockIdx.x / chunks;
-        if (t >= rows) return;
-        hh = (blockIdx.x % chunks) * R + rl;
+        t = x / chunks;
+        if (t >= sp.rows) return;
+        hh = (x - t * chunks) * R + rl;
         valid = hh < a.G;
         if (!valid) hh = a.G - 1;
         compact_list(a.lists + ((size_t)t * a.Hkv + g) * a.n_sel, a.n_sel, a.nb, a.tail, lst + 2, lst);
@@ -627,8 +649,8 @@ __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a
         seq = a.row_seq[t];
         own = last_own = a.row_pos[t] - a.T;
     } else {
-        if ((int)blockIdx.x >= a.counts[1]) return;
-        const BatchTile tl = a.tiles[blockIdx.x];
+        if (x >= sp.row_tiles) return;
+        const BatchTile tl = a.tiles[x];
         const int n_th = tl.n_new * a.G, last = min(tl.row0 + R, n_th) - 1;
         const int rq0 = tl.row0 + rl;
         valid = rq0 < n_th;
@@ -640,17 +662,72 @@ __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a
         own = tl.past + tr;
         last_own = tl.past + last / a.G;
     }
-    const int h = g * a.G + hh;
-    const uint32_t orow = (uint32_t)t * a.H + h;
-    auto id_of = [&](int c) {
+    const uint32_t orow = (uint32_t)t * a.H + g * a.G + hh;
+    float *out = a.out, *lse = a.lse;
+    if (n_split > 1) {
+        const size_t part = (size_t)split * sp.rows * a.H;
+        out = a.part_o + part * D;
+        lse = a.part_l + part;
+    }
+    // (a row that sees no key of the split: output 0, log-sum-exp -inf)
+    const int key0 = split * kps, n_keys = min(kps, n_ctx + last_own + 1 - key0);
+    if (n_keys <= 0) {
+        if (valid && threadIdx.x < R) lse[orow] = -INFINITY;
+        return;
+    }
+    auto id_of = [&](int c0) {
+        const int c = c0 + key0;
         if (c >= n_ctx) return c - n_ctx;
         if constexpr (LIST) return ~list_key(c, lst + 2, lst[0], a.bshift, a.nb, a.tail);
         else return ~c;
     };
     const int64_t sb = seq * a.s_ss + g * a.s_sh;
-    attn_f32_rows<D, R>(sm, a.ks + sb, a.vs + sb, a.s_st, a.kc + g * a.c_sh, a.vc + g * a.c_sh,
-                        a.c_st, id_of, n_ctx + last_own + 1, a.q + (size_t)orow * D, n_ctx + own,
-                        a.scale, valid, a.out, a.lse, orow);
+    attn_f32_rows<D, R, 4>(sm, a.ks + sb, a.vs + sb, a.s_st, a.kc + g * a.c_sh, a.vc + g * a.c_sh,
+                           a.c_st, id_of, n_keys, a.q + (size_t)orow * D,
+                           max(-1, min(n_keys - 1, n_ctx + own - key0)), a.scale, valid, out, lse, orow);
+}
+
+// One wave per (token, head): lane s takes split s's log-sum-exp, D/4 lanes (twice at d 64) then
+// add the splits' outputs.
+template <int D, bool LIST>
+__global__ __launch_bounds__(256) void batch_merge_f32(BaF32Args a) {
+    constexpr int LPR = D / 4, NG = 64 / LPR;
+    const int lane = threadIdx.x & 63, grp = lane / LPR, col = lane % LPR;
+    const long th = blockIdx.x * 4l + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const BatchSplit sp = load_split(a.counts);
+    int n, kps;
+    f32_split<LIST>(a, sp, n, kps);
+    const long rows = (long)sp.rows * a.H;
+    if (n == 1 || th >= rows) return;
+    float M = -INFINITY;
+    for (int s = lane; s < n; s += 64) M = fmaxf(M, a.part_l[s * rows + th]);
+    M = wave_max(M);
+    const float ref = M == -INFINITY ? 0.f : M;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float z = 0.f;
+    for (int c0 = 0; c0 < n; c0 += 64) {
+        const float w = c0 + lane < n ? expf(a.part_l[(c0 + lane) * rows + th] - ref) : 0.f;
+        z += w;
+        const int m = min(64, n - c0);
+#pragma unroll 4
+        for (int j0 = 0; j0 < m; j0 += NG) {
+            const int j = min(j0 + grp, m - 1);
+            float wj = __shfl(w, j, 64);
+            wj = j0 + grp < m ? wj : 0.f;
+            const f32x4 v = *(const f32x4*)(a.part_o + ((c0 + j) * rows + th) * D + col * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)                  // (weight 0: the output may not be written)
+                acc[i] = wj != 0.f ? fmaf(wj, v[i], acc[i]) : acc[i];
+        }
+    }
+    z = wave_sum(z);
+#pragma unroll
+    for (int o = LPR; o < 64; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], o, 64);
+    const float inv = M == -INFINITY ? 0.f : 1.0f / z;
+    if (grp == 0) *(f32x4*)(a.out + th * D + col * 4) = acc * inv;
+    if (a.lse && lane == 0) a.lse[th] = M == -INFINITY ? M : M + logf(z);
 }
 
 }  // namespace
@@ -659,8 +736,18 @@ __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a
 // has room for is split further, up to kBaWgs workgroups of kBaRows rows.
 BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_batch& b, int n_sel) {
     BatchAttnWorkspace w = {};
-    if (p.dtype != RELAXKV_DTYPE_BF16 || b.n_rows == 0) return w;
+    if (b.n_rows == 0) return w;
     const long G = p.H / p.H_kv, rows = (long)b.n_rows * p.H;
+    if (p.dtype == RELAXKV_DTYPE_F32) {
+        // (with more than one split, kBaF32Wgs workgroups of kBatchRowsF32 rows at most)
+        const long items = (n_sel == 0 ? (long)b.tile_cap
+                                       : b.n_rows * ((G + kBatchRowsF32 - 1) / kBatchRowsF32)) * p.H_kv;
+        const size_t parts = (size_t)kBaF32Wgs * kBatchRowsF32;
+        w.ctx_wgs = (int)(items > kBaF32Wgs ? items : kBaF32Wgs);
+        w.part_s_off = parts * p.d * 4;
+        w.total = w.part_s_off + parts * 4;
+        return w;
+    }
     const long least = (long)kBaWgs * kBaRows;
     const long item_cap = (b.n_rows * G + kBaRows - 1) / kBaRows * p.H_kv;
     const long list_items = (long)b.n_rows * p.H_kv * ((G + kBaRows - 1) / kBaRows);
@@ -716,18 +803,26 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
         a.scale = scale;
         a.out = (float*)out;
         a.lse = lse_out;
-        const int chunks = (G + kBatchRowsF32 - 1) / kBatchRowsF32;
-        const unsigned gx = list ? (unsigned)(b.n_rows * chunks) : (unsigned)b.tile_cap;
-        auto go = [&](auto kernel, size_t lds) {
-            hipLaunchKernelGGL(kernel, dim3(gx, p.H_kv), dim3(MfmaF32<16>::waves * 64),
-                               lds + (list ? (n_sel + 2) * sizeof(int) : 0), st, a);
+        const BatchAttnWorkspace w = batch_attn_layout(p, b, n_sel);
+        a.list_items = p.H_kv * ((G + kBatchRowsF32 - 1) / kBatchRowsF32);
+        a.list_tiles = (int)(((long)n_sel * block + kBaF32Keys - 1) / kBaF32Keys);
+        a.part_o = (float*)ws;
+        a.part_l = (float*)(ws + w.part_s_off);
+        auto go = [&](auto d_t, auto list_t) {
+            constexpr int D = decltype(d_t)::value;
+            constexpr bool LIST = decltype(list_t)::value;
+            hipLaunchKernelGGL((battn_f32<D, LIST>), dim3(w.ctx_wgs), dim3(MfmaF32<16>::waves * 64),
+                               sizeof(AttnF32Lds<D, kBatchRowsF32>) + (LIST ? (n_sel + 2) * sizeof(int) : 0),
+                               st, a);
+            hipLaunchKernelGGL((batch_merge_f32<D, LIST>), dim3((unsigned)(((long)b.n_rows * p.H + 3) / 4)),
+                               dim3(256), 0, st, a);
         };
         if (p.d == 128) {
-            if (list) go(battn_f32<128, true>, sizeof(AttnF32Lds<128, 16>));
-            else go(battn_f32<128, false>, sizeof(AttnF32Lds<128, 16>));
+            if (list) go(Int<128>{}, Int<1>{});
+            else go(Int<128>{}, Int<0>{});
         } else {
-            if (list) go(battn_f32<64, true>, sizeof(AttnF32Lds<64, 16>));
-            else go(battn_f32<64, false>, sizeof(AttnF32Lds<64, 16>));
+            if (list) go(Int<64>{}, Int<1>{});
+            else go(Int<64>{}, Int<0>{});
         }
         return hipGetLastError();
     }

@@ -40,11 +40,39 @@ def test_shared(gpu_lib, name, dtype):
     s.check(s.reference(), name)
 
 
-def test_shared_many_splits(gpu_lib):
-    """Few rows over a long context: many key splits, an uneven last one."""
-    s = Step(past=[17], new=[1], T=20011, H=4, H_kv=1, d=64, seed=3)
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("T,H,H_kv,d,past,new", [
+    (20011, 4, 1, 64, [17], [1]),             # few rows over a long context: many key splits
+    (9000, 3, 3, 128, [400], [2]),            # the last split ends in the suffix, causally
+    (2560, 8, 8, 64, [256 * 3 - 1, 5], [2, 1]),   # a row that sees nothing of the last split
+    (5000, 16, 2, 128, [3] * 30, [1] * 30),   # two chunks of rows, several splits each
+    (700, 16, 2, 128, [0] * 90, [3] * 90),    # chunks cut anywhere
+    (96, 32, 8, 64, [0, 1], [400, 300]),      # many chunks over a short context
+])
+def test_shared_splits(gpu_lib, T, H, H_kv, d, past, new, dtype):
+    if dtype == F32 and sum(new) > 100:
+        new = [max(1, n // 5) for n in new]
+    s = Step(past=past, new=new, T=T, H=H, H_kv=H_kv, d=d, dtype=dtype, seed=3)
     s.shared()
     s.check(s.reference())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_room_does_not_change_the_bits(gpu_lib, dtype):
+    """The same step in a batch with room for many more rows, requests and tokens."""
+    a, b = (Step(past=[40, 3, 60], new=[1, 20, 1], T=900, dtype=dtype, seed=8, extra_rows=e, room=r)
+            for e, r in ((0, 70), (900, 3000)))
+    for s in (a, b):
+        s.ks[:, :, 63:], s.vs[:, :, 63:] = 0, 0
+    b.ks[:, :, :63], b.vs[:, :, :63] = a.ks[:, :, :63], a.vs[:, :, :63]
+    b.kc.copy_(a.kc), b.vc.copy_(a.vc), b.q[:22].copy_(a.q)
+    for s in (a, b):
+        s.shared()
+    assert torch.equal(a.out, b.out[:22]) and torch.equal(a.lse, b.lse[:22])
+    lists = torch.arange(9, dtype=torch.int32, device="cuda").expand(922, 2, 9).contiguous()
+    a.blocks(64, lists[:22])
+    b.blocks(64, lists)
+    assert torch.equal(a.out, b.out[:22]) and torch.equal(a.lse, b.lse[:22])
 
 
 def test_shared_one_key_is_exact(gpu_lib):
