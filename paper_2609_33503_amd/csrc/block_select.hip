@@ -13,7 +13,7 @@
 // per row and KV head, against 4 G d per key of the attention that follows.
 //
 // block_means is memory bound (reads every key once); the scores' products are few, and the
-// top-k of up to 4096 blocks searches the bits of the k-th key over keys in registers.
+// top-k of up to 4096 blocks keeps its keys in registers.
 
 #include <algorithm>
 
@@ -167,76 +167,94 @@ __device__ __forceinline__ uint32_t score_key(float f) {
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Sum over the wave's lanes, as a uniform value.
-__device__ __forceinline__ uint32_t wave_total(uint32_t x) {
-    x += __builtin_amdgcn_update_dpp(0u, x, 0x111, 0xf, 0xf, true);    // row_shr:1, 2, 4, 8
-    x += __builtin_amdgcn_update_dpp(0u, x, 0x112, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0u, x, 0x114, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0u, x, 0x118, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0u, x, 0x142, 0xa, 0xf, true);    // row_bcast:15, 31
-    x += __builtin_amdgcn_update_dpp(0u, x, 0x143, 0xc, 0xf, true);
-    return __builtin_amdgcn_readlane(x, 63);
+// Inclusive prefix sum over the wave's lanes.
+__device__ __forceinline__ int wave_scan_dpp(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);     // row_shr:1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);     // row_bcast:15, 31
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);
+    return x;
 }
 
 // One workgroup of W waves per (row, KV head): wave w holds the 8 * 64 blocks from w * 512,
-// block e * 64 + lane of them in register e.  The k-th largest key is the largest t with at
-// least k keys >= t, found two bits at a time: the three counts that decide a step are at
-// most 512 per wave and go through the wave's sum packed in 10 bits each, then through LDS.
-// (2048 blocks, k 32, 64 rows of KV heads: 4.6 us; one wave per row and one bit at a time by
-// ballots, which the scalar unit counts, 42 us.)  Blocks past nb hold key 0; a NaN's key 0
-// lies at a lower block, and k <= nb, so none of them is ever taken.
+// block e * 64 + lane of them in register e.  The k-th largest key is found 8 bits at a time
+// from a histogram in LDS of the keys that share the bits found so far, in four copies (scores
+// share few exponents, and an atomic takes a turn per lane of the same address); the next
+// digit's histogram is cleared while this one is summed.  Blocks past nb hold key 0; a NaN's key
+// 0 lies at a lower block, and k <= nb, so none of them is ever taken.
+// (2048 blocks, 64 rows of KV heads, k 32: 6.7 us; two bits at a time by counting keys in every
+// wave 11.4, one wave per row and one bit at a time by ballots 42.)
 template <int W>
 __global__ __launch_bounds__(W * 64) void block_topk_reg(const float* __restrict__ scores, int nb,
                                                          int k, const int32_t* __restrict__ counts,
                                                          int n_rows, int Hkv,
                                                          int32_t* __restrict__ out) {
-    constexpr int E = 8;
-    __shared__ uint32_t part[2][W];
+    constexpr int E = 8, NT = W * 64, COPIES = 4;
+    constexpr int SW = W < 4 ? W : 4, BPT = 256 / (SW * 64);   // waves that sum, bins per thread
+    __shared__ int hist[2][COPIES][256];
+    __shared__ int wsum[SW], found[2];
+    __shared__ uint32_t part[W];
     const long unit = blockIdx.x;
-    const int lane = threadIdx.x & 63;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (unit >= (long)min(counts[0], n_rows) * Hkv) return;
-    const float* s = scores + unit * nb;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const float* s = scores + unit * nb;                 // (within the workspace for every unit)
     const int i0 = w * (E * 64) + lane;
     uint32_t key[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) key[e] = i0 + e * 64 < nb ? score_key(s[i0 + e * 64]) : 0u;
-    // The sum over the workgroup of three counts of at most 512 per wave (c in 10-bit fields).
-    auto total3 = [&](uint32_t c, int turn, int& n1, int& n2, int& n3) {
-        c = wave_total(c);
-        if constexpr (W == 1) {
-            n1 = c & 1023;
-            n2 = c >> 10 & 1023;
-            n3 = c >> 20;
-        } else {
-            if (lane == 0) part[turn & 1][w] = c;
-            __syncthreads();
-            n1 = n2 = n3 = 0;
+    for (int e = 0; e < E; ++e) key[e] = i0 + e * 64 < nb ? __float_as_uint(s[i0 + e * 64]) : 0xffffffffu;
+    if (unit >= (long)min(counts[0], n_rows) * Hkv) return;
+    for (int i = tid; i < COPIES * 256; i += NT) hist[0][0][i] = 0;
 #pragma unroll
-            for (int x = 0; x < W; ++x) {
-                const uint32_t p = part[turn & 1][x];
-                n1 += p & 1023;
-                n2 += p >> 10 & 1023;
-                n3 += p >> 20;
+    for (int e = 0; e < E; ++e) key[e] = score_key(__uint_as_float(key[e]));   // (past nb: a NaN's)
+    __syncthreads();
+    uint32_t t = 0;
+    int need = k;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        const int shift = 24 - 8 * d, cur = d & 1;
+        int (*h)[256] = hist[cur];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (d == 0 || key[e] >> (shift + 8) == t >> (shift + 8))
+                atomicAdd(&h[lane & (COPIES - 1)][key[e] >> shift & 255], 1);
+        __syncthreads();
+        if (d < 3)
+            for (int i = tid; i < COPIES * 256; i += NT) hist[cur ^ 1][0][i] = 0;
+        // Thread i sums the bins from 255 - i * BPT downwards.
+        int c[BPT], sum = 0, incl = 0;
+        if (w < SW) {
+#pragma unroll
+            for (int j = 0; j < BPT; ++j) {
+                const int bin = 255 - tid * BPT - j;
+                c[j] = h[0][bin] + h[1][bin] + h[2][bin] + h[3][bin];
+                sum += c[j];
+            }
+            incl = wave_scan_dpp(sum);
+            if (SW > 1 && lane == 63) wsum[w] = incl;
+        }
+        if (SW > 1) __syncthreads();
+        if (w < SW) {
+            int before = incl - sum;
+            if (SW > 1)
+#pragma unroll
+                for (int x = 0; x < SW; ++x) before += x < w ? wsum[x] : 0;
+#pragma unroll
+            for (int j = 0; j < BPT; ++j) {
+                if (before < need && before + c[j] >= need) {
+                    found[0] = 255 - tid * BPT - j;
+                    found[1] = before;
+                }
+                before += c[j];
             }
         }
-    };
-    uint32_t t = 0;
-#pragma unroll 1
-    for (int bit = 30; bit >= 0; bit -= 2) {
-        uint32_t c1 = 0, c2 = 0, c3 = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            c1 += key[e] >= (t | 1u << bit);
-            c2 += key[e] >= (t | 2u << bit);
-            c3 += key[e] >= (t | 3u << bit);
-        }
-        int n1, n2, n3;
-        total3(c1 | c2 << 10 | c3 << 20, bit >> 1, n1, n2, n3);
-        t |= (n3 >= k ? 3u : n2 >= k ? 2u : n1 >= k ? 1u : 0u) << bit;
+        __syncthreads();
+        t |= (uint32_t)found[0] << shift;
+        need -= found[1];
     }
     // Every key above t, and of those equal to it the first `need`; in block order.
-    int gt0 = 0, eq0 = 0, above = 0;
+    int gt0 = 0, eq0 = 0;
     uint64_t mg[E], me[E];
     uint32_t own = 0;
 #pragma unroll
@@ -245,20 +263,16 @@ __global__ __launch_bounds__(W * 64) void block_topk_reg(const float* __restrict
         me[e] = __ballot(key[e] == t);
         own += (uint32_t)__popcll(mg[e]) | (uint32_t)__popcll(me[e]) << 16;
     }
-    if constexpr (W == 1) {
-        above = own & 0xffff;
-    } else {
-        if (lane == 0) part[1][w] = own;               // (the last turn above used part[0])
+    if constexpr (W > 1) {
+        if (lane == 0) part[w] = own;
         __syncthreads();
 #pragma unroll
         for (int x = 0; x < W; ++x) {
-            const uint32_t p = part[1][x];
-            above += p & 0xffff;
-            gt0 += x < w ? p & 0xffff : 0;
-            eq0 += x < w ? p >> 16 : 0;
+            const uint32_t p = x < w ? part[x] : 0u;
+            gt0 += p & 0xffff;
+            eq0 += p >> 16;
         }
     }
-    const int need = k - above;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int gt = gt0 + lanes_below(mg[e]), eq = eq0 + lanes_below(me[e]);
