@@ -367,6 +367,9 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
             if (x + kBaRing < KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             else __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
+        // The softmax before other waves' matrix products: the vector unit is the busier one (the
+        // reverse order, or none, takes 3-4% longer).
+        __builtin_amdgcn_s_setprio(1);
         if (c0 + TK > open) {                          // the run's tail, or the causal future
             const int e = lim4 - c0;
 #pragma unroll
@@ -423,6 +426,7 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
             l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 4, 5), one2, l0, false);
             l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 6, 7), one2, l1, false);
         }
+        __builtin_amdgcn_s_setprio(0);
         // O^T += V^T P^T
 #pragma unroll
         for (int y = 0; y < 2 * DB; ++y) {
@@ -489,7 +493,7 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
 // LN lanes per (token, head): its partials are the context's in order, then the suffix splits
 // that hold one of the row's keys.  Lane i takes the statistics of partial i (then i + LN, ..);
 // the outputs are loaded by groups of D/8 lanes, partial by partial in turn, four each at a
-// time with the weights handed round, so a row waits for memory about three times.
+// time with the weights handed round, so a row waits for memory about twice.
 template <int D, bool LIST, int LN>
 __device__ __forceinline__ void merge_row(const BaArgs& a, const BatchSplit& sp, long th,
                                           uint16_t* __restrict__ out, float* __restrict__ lse) {
@@ -504,7 +508,6 @@ __device__ __forceinline__ void merge_row(const BaArgs& a, const BatchSplit& sp,
     const int t = real ? t0 : 0, h = real ? (int)(th - (long)t0 * a.H) : 0;
     const int g = h / a.G, rho = t * a.G + (h - g * a.G);
     const size_t R = (size_t)sp.rows * a.G;
-    const int n_suf = (a.row_pos[t] - a.T) / sp.suf_kps + 1;
     int n_ctx;
     size_t first, step;                                  // context partial s: first + s * step
     if constexpr (LIST) {
@@ -521,10 +524,18 @@ __device__ __forceinline__ void merge_row(const BaArgs& a, const BatchSplit& sp,
         step = kBaRows;
     }
     const size_t suf = a.suf_part + (size_t)g * R + rho, suf_step = (size_t)a.Hkv * R;
-    const int n = n_ctx + n_suf;
     auto at = [&](int s) { return s < n_ctx ? first + s * step : suf + (s - n_ctx) * suf_step; };
+    // The first statistics and outputs are loaded beside the row's position, which says how many
+    // suffix splits there are: up to all of them (what a split did not write gets weight 0).
+    const int n_all = n_ctx + sp.suf_n;
     const float4 none = {-INFINITY, 0.f, 0.f, 0.f};
-    const float4 st0 = lane < n ? a.part_s[at(lane)] : none;
+    float4 st0 = a.part_s[at(min(lane, n_all - 1))];
+    f16x8 v0[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        v0[u] = *(const f16x8*)(a.part_o + at(min(u * NG + grp, n_all - 1)) * D + col * 8);
+    const int n = n_ctx + (a.row_pos[t] - a.T) / sp.suf_kps + 1;
+    st0 = lane < n ? st0 : none;
     float M = st0.x;
     for (int s = lane + LN; s < n; s += LN) M = fmaxf(M, a.part_s[at(s)].x);
 #pragma unroll
@@ -545,7 +556,8 @@ __device__ __forceinline__ void merge_row(const BaArgs& a, const BatchSplit& sp,
             for (int u = 0; u < U; ++u) {
                 const int j = j0 + u * NG + grp;
                 wj[u] = __shfl(wt, base + (j & (LN - 1)), 64);
-                v[u] = *(const f16x8*)(a.part_o + at(min(c0 + j, n - 1)) * D + col * 8);
+                v[u] = c0 + j0 == 0 ? v0[u]
+                                    : *(const f16x8*)(a.part_o + at(min(c0 + j, n - 1)) * D + col * 8);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -576,10 +588,10 @@ __device__ __forceinline__ void merge_row(const BaArgs& a, const BatchSplit& sp,
     if (lse && lane == 0) lse[th] = M == -INFINITY ? -INFINITY : (M + __log2f(ze)) * kLn2;
 }
 
-// A row takes a wave where that makes one round of waves, and where it has many partials (9
-// partials of 256 rows: 4.4 us, 5.7 with D/8 lanes per row; 33 of 2440: 9.0, 10.2); else D/8
-// lanes (5 partials of 24352 rows: 12.3 us, 20.7 with a wave).
-constexpr int kBaManyPartials = 16, kBaWaveRows = 8192;
+// A row takes a wave where it has many partials, or several and few rows (33 partials of 2440
+// rows: 9.0 us, 10.2 with D/8 lanes per row; 9 of 256: 4.4, 5.7); else D/8 lanes (5 partials of
+// 24352 rows: 12.3 us, 20.7 with a wave; 4 of 2328: 4.1, 6.3).
+constexpr int kBaManyPartials = 16, kBaSomePartials = 8, kBaFewRows = 4096;
 template <int D, bool LIST>
 __global__ __launch_bounds__(256) void batch_merge(BaArgs a, uint16_t* __restrict__ out,
                                                    float* __restrict__ lse) {
@@ -588,7 +600,8 @@ __global__ __launch_bounds__(256) void batch_merge(BaArgs a, uint16_t* __restric
     int n_ctx, kps;
     if constexpr (LIST) list_split(a, sp.rows, n_ctx, kps);
     else n_ctx = sp.tiles / sp.quota + 1;
-    if (n_ctx + sp.suf_n > kBaManyPartials || sp.rows * a.H <= kBaWaveRows)
+    const int n = n_ctx + sp.suf_n;
+    if (n > kBaManyPartials || (n >= kBaSomePartials && sp.rows * a.H <= kBaFewRows))
         merge_row<D, LIST, 64>(a, sp, blockIdx.x * 4l + (threadIdx.x >> 6), out, lse);
     else
         merge_row<D, LIST, LPR>(a, sp, (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR, out, lse);

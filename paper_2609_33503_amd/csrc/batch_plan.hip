@@ -19,23 +19,6 @@ namespace {
 constexpr int kPlanThreads = 256;
 constexpr int kPlanSeqs = 64;          // requests per workgroup
 
-__device__ __forceinline__ long block_sum(long v, long* scratch) {
-    v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return scratch[0] + scratch[1] + scratch[2] + scratch[3];
-}
-
-__device__ __forceinline__ int block_max(int v, long* scratch) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = max(v, __shfl_xor(v, o, 64));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return (int)max(max(scratch[0], scratch[1]), max(scratch[2], scratch[3]));
-}
-
 // The last entry of the ascending off[0 .. kPlanSeqs] that is <= x (x < off[kPlanSeqs]).
 __device__ __forceinline__ int owner(const int* off, int x) {
     int lo = 0;
@@ -50,7 +33,7 @@ __global__ __launch_bounds__(kPlanThreads) void batch_plan_rows(
     int n_rows, int max_suffix, int T, int G, int Hkv, int tile_rows, int32_t* __restrict__ row_off,
     int32_t* __restrict__ row_seq, int32_t* __restrict__ row_pos, BatchTile* __restrict__ tiles,
     int32_t* __restrict__ counts) {
-    __shared__ long sums[4];
+    __shared__ long sums[4][6];
     __shared__ int off[kPlanSeqs + 1], toff[kPlanSeqs + 1], past_s[kPlanSeqs];
     const int tid = threadIdx.x, first = blockIdx.x * kPlanSeqs;
     // A length is bad below 0, past the suffix room, or past the rows of the step.
@@ -76,13 +59,26 @@ __global__ __launch_bounds__(kPlanThreads) void batch_plan_rows(
             tbefore += t;
         }
     }
-    total = block_sum(total, sums);
-    bad = block_sum(bad, sums) + (total > n_rows);
-    before = block_sum(before, sums);
-    tbefore = block_sum(tbefore, sums);
-    ttotal = block_sum(ttotal, sums);
-    longest = block_max(longest, sums);
-    if (bad) total = before = tbefore = ttotal = longest = 0;
+    long part[6] = {total, ttotal, before, tbefore, bad, longest};
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) {
+            const long other = __shfl_xor(part[i], o, 64);
+            part[i] = i < 5 ? part[i] + other : max(part[i], other);
+        }
+    if ((tid & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) sums[tid >> 6][i] = part[i];
+    __syncthreads();
+    auto sum = [&](int i) { return sums[0][i] + sums[1][i] + sums[2][i] + sums[3][i]; };
+    total = sum(0);
+    bad = sum(4) + (total > n_rows);
+    if (bad) total = 0;
+    ttotal = bad ? 0 : sum(1);
+    before = bad ? 0 : sum(2);
+    tbefore = bad ? 0 : sum(3);
+    longest = bad ? 0 : (int)max(max(sums[0][5], sums[1][5]), max(sums[2][5], sums[3][5]));
     if (tid < kPlanSeqs) {                       // wave 0: one request per lane
         const int b = first + tid;
         int n = 0, p = 0;
@@ -100,9 +96,10 @@ __global__ __launch_bounds__(kPlanThreads) void batch_plan_rows(
             counts[1] = (int)ttotal;
             counts[2] = longest;
             counts[3] = bad ? RELAXKV_BATCH_ERR_LENGTHS : 0;
-            *(BatchSplit*)(counts + kBatchSplitAt) = batch_split((int)total, (int)ttotal, longest, T, G, Hkv);
         }
     }
+    if (blockIdx.x == 0 && tid == kPlanThreads - 1)      // (beside wave 0's scan)
+        *(BatchSplit*)(counts + kBatchSplitAt) = batch_split((int)total, (int)ttotal, longest, T, G, Hkv);
     __syncthreads();
     const int rows = off[kPlanSeqs], nt = toff[kPlanSeqs];
     for (int r = tid; r < rows; r += kPlanThreads) {

@@ -104,12 +104,12 @@ __global__ __launch_bounds__(256) void block_scores(const T* __restrict__ q,
     constexpr int NT = kScoreTokens;
     __shared__ __attribute__((aligned(16))) double qs[NT][D];
     const int tid = threadIdx.x, g = blockIdx.y, t0 = blockIdx.z * NT;
-    const int rows = min(counts[0], n_rows);
-    if (t0 >= rows) return;
     const int part = tid & 3, b = blockIdx.x * 64 + (tid >> 2);
     const T* m = means + ((size_t)g * nb + min(b, nb - 1)) * D;
     float mf[8];
     load8<T>(m + part * 8, mf);
+    const int rows = min(counts[0], n_rows);
+    if (t0 >= rows) return;
     // The summed group queries: 8 elements of one row per thread, the heads' loads in flight
     // together.
     for (int x = tid; x < NT * D / 8; x += 256) {
@@ -178,50 +178,44 @@ __device__ __forceinline__ int wave_scan_dpp(int x) {
     return x;
 }
 
-// One workgroup of W waves per (row, KV head): wave w holds the 8 * 64 blocks from w * 512,
-// block e * 64 + lane of them in register e.  The k-th largest key is found 8 bits at a time
-// from a histogram in LDS of the keys that share the bits found so far, in four copies (scores
-// share few exponents, and an atomic takes a turn per lane of the same address); the next
-// digit's histogram is cleared while this one is summed.  Blocks past nb hold key 0; a NaN's key
-// 0 lies at a lower block, and k <= nb, so none of them is ever taken.
-// (2048 blocks, 64 rows of KV heads, k 32: 6.7 us; two bits at a time by counting keys in every
+// The k largest of a row's keys, by a workgroup of W waves: wave w holds the 8 * 64 blocks from
+// w * 512, block e * 64 + lane of them in register e.  The k-th largest key is found 8 bits at
+// a time from a histogram in LDS of the keys that share the bits found so far, in four copies
+// (scores share few exponents, and an atomic takes a turn per lane of the same address); the
+// next digit's histogram is cleared while this one is summed.  Blocks past the row's end hold
+// key 0; a NaN's key 0 lies at a lower block, and k is at most the row's length, so none of
+// them is ever taken.
+// (2048 blocks, 64 rows of KV heads, k 32: 5.6 us; two bits at a time by counting keys in every
 // wave 11.4, one wave per row and one bit at a time by ballots 42.)
 template <int W>
-__global__ __launch_bounds__(W * 64) void block_topk_reg(const float* __restrict__ scores, int nb,
-                                                         int k, const int32_t* __restrict__ counts,
-                                                         int n_rows, int Hkv,
-                                                         int32_t* __restrict__ out) {
-    constexpr int E = 8, NT = W * 64, COPIES = 4;
+struct TopkLds {
+    int hist[2][4][256];
+    int wsum[4], found[2];
+    uint32_t part[W];
+};
+
+template <int W, int NT = W * 64>          // (NT: threads of the workgroup)
+__device__ __forceinline__ void topk_keys(TopkLds<W>& sm, const uint32_t (&key)[8], int k, int32_t* out) {
+    constexpr int E = 8, COPIES = 4;
     constexpr int SW = W < 4 ? W : 4, BPT = 256 / (SW * 64);   // waves that sum, bins per thread
-    __shared__ int hist[2][COPIES][256];
-    __shared__ int wsum[SW], found[2];
-    __shared__ uint32_t part[W];
-    const long unit = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const float* s = scores + unit * nb;                 // (within the workspace for every unit)
     const int i0 = w * (E * 64) + lane;
-    uint32_t key[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) key[e] = i0 + e * 64 < nb ? __float_as_uint(s[i0 + e * 64]) : 0xffffffffu;
-    if (unit >= (long)min(counts[0], n_rows) * Hkv) return;
-    for (int i = tid; i < COPIES * 256; i += NT) hist[0][0][i] = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) key[e] = score_key(__uint_as_float(key[e]));   // (past nb: a NaN's)
+    for (int i = tid; i < COPIES * 256; i += NT) sm.hist[0][0][i] = 0;
     __syncthreads();
     uint32_t t = 0;
     int need = k;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
         const int shift = 24 - 8 * d, cur = d & 1;
-        int (*h)[256] = hist[cur];
+        int (*h)[256] = sm.hist[cur];
 #pragma unroll
         for (int e = 0; e < E; ++e)
-            if (d == 0 || key[e] >> (shift + 8) == t >> (shift + 8))
+            if (w < W && (d == 0 || key[e] >> (shift + 8) == t >> (shift + 8)))
                 atomicAdd(&h[lane & (COPIES - 1)][key[e] >> shift & 255], 1);
         __syncthreads();
         if (d < 3)
-            for (int i = tid; i < COPIES * 256; i += NT) hist[cur ^ 1][0][i] = 0;
+            for (int i = tid; i < COPIES * 256; i += NT) sm.hist[cur ^ 1][0][i] = 0;
         // Thread i sums the bins from 255 - i * BPT downwards.
         int c[BPT], sum = 0, incl = 0;
         if (w < SW) {
@@ -232,26 +226,26 @@ __global__ __launch_bounds__(W * 64) void block_topk_reg(const float* __restrict
                 sum += c[j];
             }
             incl = wave_scan_dpp(sum);
-            if (SW > 1 && lane == 63) wsum[w] = incl;
+            if (SW > 1 && lane == 63) sm.wsum[w] = incl;
         }
         if (SW > 1) __syncthreads();
         if (w < SW) {
             int before = incl - sum;
             if (SW > 1)
 #pragma unroll
-                for (int x = 0; x < SW; ++x) before += x < w ? wsum[x] : 0;
+                for (int x = 0; x < SW; ++x) before += x < w ? sm.wsum[x] : 0;
 #pragma unroll
             for (int j = 0; j < BPT; ++j) {
                 if (before < need && before + c[j] >= need) {
-                    found[0] = 255 - tid * BPT - j;
-                    found[1] = before;
+                    sm.found[0] = 255 - tid * BPT - j;
+                    sm.found[1] = before;
                 }
                 before += c[j];
             }
         }
         __syncthreads();
-        t |= (uint32_t)found[0] << shift;
-        need -= found[1];
+        t |= (uint32_t)sm.found[0] << shift;
+        need -= sm.found[1];
     }
     // Every key above t, and of those equal to it the first `need`; in block order.
     int gt0 = 0, eq0 = 0;
@@ -264,23 +258,110 @@ __global__ __launch_bounds__(W * 64) void block_topk_reg(const float* __restrict
         own += (uint32_t)__popcll(mg[e]) | (uint32_t)__popcll(me[e]) << 16;
     }
     if constexpr (W > 1) {
-        if (lane == 0) part[w] = own;
+        if (w < W && lane == 0) sm.part[w] = own;
         __syncthreads();
 #pragma unroll
         for (int x = 0; x < W; ++x) {
-            const uint32_t p = x < w ? part[x] : 0u;
+            const uint32_t p = x < w ? sm.part[x] : 0u;
             gt0 += p & 0xffff;
             eq0 += p >> 16;
         }
     }
+    if (w >= W) return;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int gt = gt0 + lanes_below(mg[e]), eq = eq0 + lanes_below(me[e]);
-        if (key[e] > t || (key[e] == t && eq < need)) out[unit * k + gt + min(eq, need)] = i0 + e * 64;
+        if (key[e] > t || (key[e] == t && eq < need)) out[gt + min(eq, need)] = i0 + e * 64;
         gt0 += __popcll(mg[e]);
         eq0 += __popcll(me[e]);
     }
 }
+
+// One workgroup per (row, KV head) over scores in memory.
+template <int W>
+__global__ __launch_bounds__(W * 64) void block_topk_reg(const float* __restrict__ scores, int nb,
+                                                         int k, const int32_t* __restrict__ counts,
+                                                         int n_rows, int Hkv,
+                                                         int32_t* __restrict__ out) {
+    __shared__ TopkLds<W> sm;
+    const long unit = blockIdx.x;
+    const int i0 = (threadIdx.x >> 6) * 512 + (threadIdx.x & 63);
+    const float* s = scores + unit * nb;                 // (within the workspace for every unit)
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = i0 + e * 64 < nb ? s[i0 + e * 64] : 0.f;
+    if (unit >= (long)min(counts[0], n_rows) * Hkv) return;
+    uint32_t key[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) key[e] = i0 + e * 64 < nb ? score_key(x[e]) : 0u;
+    topk_keys<W>(sm, key, k, out + unit * k);
+}
+
+// Scores and top-k of one (row, KV head) in one workgroup: for steps of few rows, which are
+// bound by the latency of a launch and not by a CU's 64-bit products (97 rows of 2 KV heads, 512
+// blocks, d 64: 7.1 us for 5.2 + 6.0 in two launches; but 8 rows of 8 heads, 2048 blocks, d 128:
+// 24.2 us for 6.2 + 5.6).  Four lanes per block, each a quarter of the head dimension.
+constexpr int kFusedThreads = 1024;
+template <typename T, int D, int W>
+__global__ __launch_bounds__(kFusedThreads) void block_select_rows(const T* __restrict__ q,
+                                                            const T* __restrict__ means, int nb, int k,
+                                                            const int32_t* __restrict__ counts,
+                                                            int n_rows, int H, int Hkv, int G,
+                                                            int32_t* __restrict__ out) {
+    constexpr int NT = kFusedThreads, NC = D / 32, BLK = NT / 4;   // chunks of a lane, blocks at a time
+    __shared__ TopkLds<W> sm;
+    __shared__ float score[512 * W];
+    __shared__ __attribute__((aligned(16))) double qs[D];
+    const int tid = threadIdx.x, part = tid & 3;
+    const int t = blockIdx.x / Hkv, g = blockIdx.x - t * Hkv;
+    if (t >= min(counts[0], n_rows)) return;
+    const T* m = means + (size_t)g * nb * D + part * 8;
+    float mf[NC][8];
+    auto load = [&](int b) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) load8<T>(m + (size_t)min(b, nb - 1) * D + i * 32, mf[i]);
+    };
+    load(tid >> 2);
+    for (int c = tid; c < D; c += NT) {
+        const T* p = q + ((size_t)t * H + g * G) * D + c;
+        double s = 0.0;
+#pragma unroll 4
+        for (int h = 0; h < G; ++h) {
+            if constexpr (sizeof(T) == 2) s += (double)bf16_bits_to_f32(p[h * D]);
+            else s += (double)p[h * D];
+        }
+        qs[c] = s;
+    }
+    __syncthreads();
+    for (int b0 = 0; b0 < nb; b0 += BLK) {
+        const int b = b0 + (tid >> 2);
+        double s = 0.0, s1 = 0.0;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+            asm volatile("" ::: "memory");               // (the queries are read again, not kept)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                s = fma(qs[part * 8 + i * 32 + e], (double)mf[i][e], s);
+                s1 = fma(qs[part * 8 + i * 32 + e + 1], (double)mf[i][e + 1], s1);
+            }
+        }
+        if (b0 + BLK < nb) load(b + BLK);
+        s += s1;
+        s += __shfl_xor(s, 1, 64);
+        s += __shfl_xor(s, 2, 64);
+        if (part == 0 && b < nb) score[b] = (float)s;
+    }
+    __syncthreads();
+    const int i0 = (tid >> 6) * 512 + (tid & 63);
+    uint32_t key[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) key[e] = i0 + e * 64 < nb ? score_key(score[min(i0 + e * 64, nb - 1)]) : 0u;
+    topk_keys<W, NT>(sm, key, k, out + (size_t)blockIdx.x * k);
+}
+
+// Steps that take one launch: products per row (blocks times d), and units (rows times KV
+// heads) of one round of workgroups.
+constexpr long kFusedProducts = 65536, kFusedUnits = 256;
 
 // Rows of any length: one workgroup per (row, KV head) reads its scores once per 8-bit
 // digit and once for the compaction.
@@ -372,6 +453,25 @@ hipError_t launch_block_means(const relaxkv_problem& p, int layer0, int n_layers
 hipError_t launch_block_select(const relaxkv_problem& p, const relaxkv_batch& b, int block,
                                const void* means, const void* q, int n_sel, int32_t* blocks,
                                float* scores, hipStream_t st) {
+    const int nb = block_count(p, block);
+    const long units = (long)b.n_rows * p.H_kv;
+    if ((long)nb * p.d <= kFusedProducts && units <= kFusedUnits) {
+        auto go = [&](auto kernel, auto q_t) {
+            typedef decltype(q_t) T;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3(kFusedThreads), 0, st, (const T*)q,
+                               (const T*)means, nb, n_sel, b.counts, b.n_rows, p.H, p.H_kv,
+                               p.H / p.H_kv, blocks);
+        };
+        auto go_t = [&](auto q_t) {
+            typedef decltype(q_t) T;
+            if (p.d == 128) go(block_select_rows<T, 128, 1>, q_t);
+            else if (nb <= 512) go(block_select_rows<T, 64, 1>, q_t);
+            else go(block_select_rows<T, 64, 2>, q_t);
+        };
+        if (p.dtype == RELAXKV_DTYPE_BF16) go_t(uint16_t{});
+        else go_t(float{});
+        return hipGetLastError();
+    }
     if (p.dtype == RELAXKV_DTYPE_BF16) {
         if (p.d == 128) launch_scores<uint16_t, 128>(p, b, block, means, q, scores, st);
         else launch_scores<uint16_t, 64>(p, b, block, means, q, scores, st);
@@ -379,8 +479,6 @@ hipError_t launch_block_select(const relaxkv_problem& p, const relaxkv_batch& b,
         if (p.d == 128) launch_scores<float, 128>(p, b, block, means, q, scores, st);
         else launch_scores<float, 64>(p, b, block, means, q, scores, st);
     }
-    const int nb = block_count(p, block);
-    const long units = (long)b.n_rows * p.H_kv;
     auto go = [&](auto kernel, int waves) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3(waves * 64), 0, st, scores, nb, n_sel,
                            b.counts, b.n_rows, p.H_kv, blocks);

@@ -604,12 +604,16 @@ class Request:
         n = positions.shape[0] if isinstance(positions, torch.Tensor) and positions.dim() == 1 else -1
         self._want(positions, "positions", torch.int32, (n,))
         rows = self._rows(q, k, v, n)
-        for t, o, name, heads in ((q, q_out, "q_out", self.H), (k, k_out, "k_out", self.H_kv),
-                                  (v, v_out, "v_out", self.H_kv)):
-            if o is not None:
-                self._want(o, name, self.dtype, (n, heads, self.d))
-            if (t is None) != (o is None):
-                raise ValueError(f"{name} and its input must both be given, or neither")
+        if (q is None) != (q_out is None) or (k is None) != (k_out is None) \
+                or (v is None) != (v_out is None):
+            raise ValueError("an output and its input must both be given, or neither")
+        kv_shape = (n, self.H_kv, self.d)
+        if q is not None:
+            self._want(q_out, "q_out", self.dtype, (n, self.H, self.d))
+        if k is not None:
+            self._want(k_out, "k_out", self.dtype, kv_shape)
+        if v is not None:
+            self._want(v_out, "v_out", self.dtype, kv_shape)
         _check(self._lib.relaxkv_fresh_rows(self._ref, self._rope(rope), ctypes.byref(rows),
                                             positions.data_ptr(), _ptr(q_out), _ptr(k_out),
                                             _ptr(v_out), self._here(stream)), "relaxkv_fresh_rows")
