@@ -35,6 +35,7 @@ constexpr int kBaKeys = 32;            // keys per tile
 constexpr int kBaWgs = 768;            // workgroups the splits aim for (three per CU)
 constexpr int kBaMinTiles = 8;         // fewest tiles per split
 constexpr int kBaXcds = 8;
+constexpr int kBaLongSuffix = 1024;    // tokens from which the suffix items go first
 // float32: a split's keys are at least one block for each of the 16 waves, its workgroups one
 // round (one per CU at d 128).
 constexpr int kBaF32Keys = 256, kBaF32Wgs = 256;
@@ -52,6 +53,7 @@ struct BatchSplit {
     int32_t rows, row_tiles;           // of the step
     int32_t chunks, items, tiles, len, quota, workers;
     int32_t per_item;                  // workers of an item; 0: cut anywhere
+    int32_t suffix_first;              // order of the items in the launch
     int32_t suf_n, suf_kps;            // suffix splits, keys each
     int32_t f32_n, f32_kps;            // float32: splits of a row tile's keys, keys each
 };
@@ -75,10 +77,13 @@ __host__ __device__ inline BatchSplit batch_split(int rows, int row_tiles, int l
     s.items = s.chunks * Hkv;
     s.tiles = (T + kBaKeys - 1) / kBaKeys;
     const int most = (s.tiles + kBaMinTiles - 1) / kBaMinTiles;
-    int n = s.items > 0 ? kBaWgs / s.items : 0;
+    // One chunk of rows is bound by memory, and one workgroup per CU streams better than three
+    // with a third of the keys (1-16 requests over 32K: 34-40 us, 38-44).
+    const int wgs = s.chunks == 1 ? kBaWgs / 3 : kBaWgs;
+    int n = s.items > 0 ? wgs / s.items : 0;
     n = n < most ? n : most;
     // (whole rounds of the XCDs)
-    while (n > 0 && (n * Hkv + kBaXcds - 1) / kBaXcds * kBaXcds * s.chunks > kBaWgs) --n;
+    while (n > 0 && (n * Hkv + kBaXcds - 1) / kBaXcds * kBaXcds * s.chunks > wgs) --n;
     s.per_item = n >= 6 || n == most ? n : 0;
     if (s.per_item) {
         s.quota = (s.tiles + n - 1) / n;
@@ -91,6 +96,10 @@ __host__ __device__ inline BatchSplit batch_split(int rows, int row_tiles, int l
         s.len = s.tiles;
         s.workers = (int32_t)((all + s.quota - 1) / s.quota);
     }
+    // Long suffixes are bound by memory, several chunks of rows by computation: the suffix items
+    // go first, so that the two overlap (64 requests of 1500 suffix tokens over 32K: 131 us, 150
+    // with them last); short ones go last, behind the longer items (600 tokens: 72, 75 first).
+    s.suffix_first = s.chunks > 1 && longest >= kBaLongSuffix;
     int quota;
     batch_split_keys((longest + kBaKeys - 1) / kBaKeys, row_tiles * Hkv, kBaWgs, kBaMinTiles, s.suf_n,
                      quota);

@@ -14,9 +14,10 @@
 // - How the items are split over workgroups (BatchSplit) follows from the step itself and
 //   comes with its plan, so a batch with room for many rows costs a small step nothing.
 // - Each item streams 32-key K and V tiles through three swizzled LDS buffers by direct
-//   loads; 48 KB of LDS and 163 registers let three workgroups share a CU, whose softmax,
-//   matrix products and waits overlap.  A wave owns 32 rows (one per lane): S^T = K Q^T, online
-//   softmax in the exp2 domain with a lazily raised maximum, O^T += V^T P^T.
+//   loads; 48 KB of LDS and 165 registers let three workgroups share a CU, whose softmax,
+//   matrix products and waits overlap.  A wave owns 32 rows (16 where that covers the item;
+//   one row per lane): S^T = K Q^T, online softmax in the exp2 domain with a lazily raised
+//   maximum, O^T += V^T P^T.
 // - Probabilities are rounded to bf16 for the second product (2^-9 of each, independent over
 //   keys: about as much as rounding O once; float32 products would take eight times the matrix
 //   time).  The output is divided by the sum of the rounded ones, which keeps a row that
@@ -69,7 +70,7 @@ struct BaArgs {
     float4* part_s;          // (max, sum of rounded, sum of exact probabilities, scale)
     size_t suf_part;
     int T, H, Hkv, G, n_rows, n_sel, bshift, nb, tail;
-    int ctx_wgs;             // context workgroups of the launch; the others take suffix items
+    int ctx_wgs, suf_wgs;    // workgroups of the launch for context and suffix items
     int list_tiles, list_items;   // listed: key tiles of a row at most, items of a token
     float sl2;               // softmax scale * log2(e)
 };
@@ -91,13 +92,37 @@ __device__ __forceinline__ void list_split(const BaArgs& a, int rows, int& n, in
     kps *= kBaKeys;
 }
 
-__device__ __forceinline__ float ba_pair_max(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+// MFMA blocks of NR (token, head) rows: the lane's row is lane % NR, its group lane / NR.
+// Value v of a 32-key tile's logits is key key0(v) + 4 group, value v of an output block is element
+// key0(v) + 4 group of the block's NR ones (key0: 8 (v/4) + v%4 for 32 rows, 16 (v/4) + v%4 for 16).
+template <int NR> struct RowBlock;
+template <> struct RowBlock<32> {
+    typedef f32x16 Acc;
+    static constexpr int key_sub = 1, kdim = 16;       // 32-key tile: one block of logits
+    static __device__ __forceinline__ Acc mac(bf16x8 a, bf16x8 b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+    template <typename F> static __device__ __forceinline__ float groups(float x, F f) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+};
+template <> struct RowBlock<16> {
+    typedef f32x4 Acc;
+    static constexpr int key_sub = 2, kdim = 32;       // two blocks of 16 keys
+    static __device__ __forceinline__ Acc mac(bf16x8 a, bf16x8 b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+    template <typename F> static __device__ __forceinline__ float groups(float x, F f) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        return RowBlock<32>::groups(f(__uint_as_float(r[0]), __uint_as_float(r[1])), f);
+    }
+};
+template <int NR> __device__ __forceinline__ float ba_group_max(float x) {
+    return RowBlock<NR>::groups(x, [](float a, float b) { return fmaxf(a, b); });
 }
-__device__ __forceinline__ float ba_pair_sum(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+template <int NR> __device__ __forceinline__ float ba_group_sum(float x) {
+    return RowBlock<NR>::groups(x, [](float a, float b) { return a + b; });
 }
 
 // fill_lds16 with a wave-uniform base and a 32-bit byte offset per lane.
@@ -140,8 +165,6 @@ __device__ __forceinline__ int list_key(int c, const int* lst, int nf, int bshif
 template <int D, bool LIST>
 __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
     constexpr int TK = kBaKeys, ST = kBaStages, NW = kBaWaves;
-    constexpr int KS = D / 16;             // k-steps of QK^T
-    constexpr int DB = D / 32;             // 32-wide d blocks of O^T
     constexpr int ROWB = 2 * D;            // tile row bytes
     constexpr int CH = D / 8;              // 16-byte chunks per row
     constexpr int RPI = 64 / CH;           // rows per wave-wide load
@@ -154,8 +177,10 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
     __shared__ int cnt[2];
 
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const bool ctx = (int)blockIdx.x < a.ctx_wgs;
     const BatchSplit sp = load_split(a.counts);
+    const int ctx0 = sp.suffix_first ? a.suf_wgs : 0, suf0 = sp.suffix_first ? 0 : a.ctx_wgs;
+    const bool ctx = sp.suffix_first ? (int)blockIdx.x >= a.suf_wgs : (int)blockIdx.x < a.ctx_wgs;
+    const int wg = (int)blockIdx.x - (ctx ? ctx0 : suf0);
     const size_t R = (size_t)sp.rows * a.G;              // rows of the step per KV head
 
     // Shared context: the worker's tiles x .. x_end - 1.
@@ -163,7 +188,7 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
     int64_t x = 0, x_end = 0;
     if (sp.rows == 0) return;
     if (ctx && !LIST) {
-        const int j = blockIdx.x / kBaXcds, xcd = blockIdx.x % kBaXcds;
+        const int j = wg / kBaXcds, xcd = wg % kBaXcds;   // (both counts are multiples of the XCDs)
         if (sp.per_item) {
             // (the chunks of one key range are consecutive workgroups of one XCD)
             const int pair = j / sp.chunks * kBaXcds + xcd;
@@ -181,18 +206,22 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
     // Made opaque per item, so that what is derived from it is not kept live across the loop.
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));
-    const int r32 = lane & 31, hf = lane >> 5;
     // The item: KV head g, the wave's first partial row and number of rows (consecutive ones),
     // the lane's row (token t, head hh of the group, last visible key lim), and the keys key0 ..
     // key0 + nk - 1 of a run (base pointers, stride); the first `open` of them every row sees.
+    // An item of at most 64 rows gives each wave 16 of them instead of 32: half the products and
+    // softmax of a wave, and a decoding request's few heads do not wait for 32 rows' (16 rows
+    // over 4096 listed keys each: 11.6 us, 14.1 with 32; 64 requests of 5 rows over suffixes of
+    // 300: 73.2, 76.6).
     int g, t, hh, lim, key0, nk, open, n_val;
+    bool small;
     const uint16_t *kb, *vb;
     int64_t st;
     size_t part;
     bool listed = false;
     if (ctx) {
         if constexpr (LIST) {
-            int y = blockIdx.x, list_n, list_kps;
+            int y = wg, list_n, list_kps;
             list_split(a, sp.rows, list_n, list_kps);
             const int split = y % list_n;
             y /= list_n;
@@ -206,15 +235,17 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
             t = y / a.Hkv;
             if (t >= sp.rows) return;
             compact_list(a.lists + ((size_t)t * a.Hkv + g) * a.n_sel, a.n_sel, a.nb, a.tail, lst, cnt);
-            const int h0 = chunk * kBaRows + w * 32;
-            n_val = a.G - h0;
-            hh = r32 < n_val ? h0 + r32 : 0;
+            small = a.G - chunk * kBaRows <= 64;
+            const int rw = small ? 16 : 32, r = lane & (rw - 1);
+            const int h0 = chunk * kBaRows + w * rw;
+            n_val = min(a.G - h0, rw);
+            hh = r < n_val ? h0 + r : 0;
             part = ((size_t)split * a.Hkv + g) * R + (size_t)t * a.G + h0;
             key0 = split * list_kps;
             const int n = __builtin_amdgcn_readfirstlane((cnt[0] << a.bshift) + cnt[1] * a.tail);
             nk = min(list_kps, n - key0);
             if (nk <= 0) {                               // nothing in this split
-                if (lane < min(n_val, 32)) a.part_s[part + lane] = float4{-INFINITY, 0.f, 0.f, 0.f};
+                if (lane < n_val) a.part_s[part + lane] = float4{-INFINITY, 0.f, 0.f, 0.f};
                 return;
             }
             listed = true;
@@ -224,12 +255,15 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
             x += min(left, sp.len - t0);                 // (the next item's first tile)
             if (nt <= 0) return;                         // (padding, which ends a range)
             g = item / sp.chunks;
-            const int rho0 = (item - g * sp.chunks) * kBaRows + w * 32;
-            n_val = sp.rows * a.G - rho0;
-            const int rho = r32 < n_val ? rho0 + r32 : 0;
+            const int row0 = (item - g * sp.chunks) * kBaRows;
+            small = sp.rows * a.G - row0 <= 64;
+            const int rw = small ? 16 : 32, r = lane & (rw - 1);
+            const int rho0 = row0 + w * rw;
+            n_val = min(sp.rows * a.G - rho0, rw);
+            const int rho = r < n_val ? rho0 + r : 0;
             t = rho / a.G;
             hh = rho - t * a.G;
-            part = (size_t)(worker + item) * kBaRows + w * 32;
+            part = (size_t)(worker + item) * kBaRows + w * rw;
             key0 = t0 * TK;
             nk = min(nt * TK, a.T - key0);
         }
@@ -239,7 +273,7 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
         vb = a.vc + g * a.c_sh;
         st = a.c_st;
     } else {
-        int y = blockIdx.x - a.ctx_wgs;
+        int y = wg;
         const int split = y % sp.suf_n;
         y /= sp.suf_n;
         g = y % a.Hkv;
@@ -256,9 +290,11 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
         const int last = (min(tl.row0 + kBaRows, n_th) - 1) / a.G;
         nk = min(sp.suf_kps, tl.past + last + 1 - key0);
         if (nk <= 0) return;
-        const int rq0 = tl.row0 + w * 32;
-        n_val = n_th - rq0;
-        const int rq = r32 < n_val ? rq0 + r32 : 0;
+        small = n_th - tl.row0 <= 64;
+        const int rw = small ? 16 : 32, r = lane & (rw - 1);
+        const int rq0 = tl.row0 + w * rw;
+        n_val = min(n_th - rq0, rw);
+        const int rq = r < n_val ? rq0 + r : 0;
         const int tr = rq / a.G;
         hh = rq - tr * a.G;
         t = tl.row_begin + tr;
@@ -270,25 +306,7 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
         st = a.s_st;
     }
     const bool live = n_val > 0;
-    const int lim4 = lim - 4 * hf;
     const int ntile = (nk + TK - 1) / TK;
-
-    bf16x8 qf[KS];
-    {
-        const uint16_t* qrow = a.q + ((size_t)t * a.H + g * a.G + hh) * D;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(qrow + ks * 16 + hf * 8);
-        // Consumed here, so the compiler's waits for these loads stay before the loop.
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
-    }
-    f32x16 o[DB];
-#pragma unroll
-    for (int db = 0; db < DB; ++db) o[db] = f32x16{};
-    // The row's reference maximum, what the logits are compared with, and subtracted from them.
-    float m_run = -INFINITY, thr = -INFINITY, m_ref = 0.f;
-    float l0 = 0.f, l1 = 0.f, e0 = 0.f, e1 = 0.f;        // sums of rounded and exact probabilities
-    const float inv_sl2 = 1.0f / a.sl2;
 
     // Loader: load jj = w + NW i fills tile rows jj RPI ..; lane l writes (row l / CH, chunk
     // l % CH) and fetches the chunk that belongs there.  The swizzle of a lane's rows is the
@@ -322,169 +340,207 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
         }
     };
 
-    // Fragment byte offsets: K rows r32 (+ 32 kb), chunk hf (+ 2 ks); V by transposing reads.
-    const int k_base = r32 * ROWB | ((hf ^ tile_swz<D>(r32)) << 4);
-    const int rl = 4 * (lane >> 5) + ((lane & 15) >> 2);
-    const int cl = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-    const int v_base0 = rl * ROWB | ((cl ^ tile_swz<D>(rl)) << 4) | ((lane & 1) << 3);
-    const int v_base1 = (rl + 8) * ROWB | ((cl ^ tile_swz<D>(rl + 8)) << 4) | ((lane & 1) << 3);
-    const char* kst = (const char*)tiles;
-    const uint32_t vlds = lds_addr(tiles) + ST * TK * ROWB;
+    auto run = [&](auto nr_t) {
+        constexpr int NR = decltype(nr_t)::value;
+        typedef RowBlock<NR> RB;
+        typedef typename RB::Acc Acc;
+        constexpr int NV = sizeof(Acc) / 4, KB = RB::key_sub, NS = KB * NV;   // logits of a lane
+        constexpr int KS = D / RB::kdim;               // k-steps of QK^T
+        constexpr int DB = D / NR, PK = 32 / RB::kdim; // d blocks of O^T, products of each per tile
+        constexpr int VSTEP = NR == 32 ? 8 : 16;       // keys between a lane's runs of four
+        const int row = lane & (NR - 1), grp = lane / NR;
+        const int lim4 = lim - 4 * grp;
+        bf16x8 qf[KS];
+        {
+            const uint16_t* qrow = a.q + ((size_t)t * a.H + g * a.G + hh) * D;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8*)(qrow + ks * RB::kdim + grp * 8);
+            // Consumed here, so the compiler's waits for these loads stay before the loop.
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
+        }
+        Acc o[DB];
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[db] = Acc{};
+        // The row's reference maximum, what the logits are compared with, and subtracted from them.
+        float m_run = -INFINITY, thr = -INFINITY, m_ref = 0.f;
+        float l0 = 0.f, l1 = 0.f, e0 = 0.f, e1 = 0.f;  // sums of rounded and exact probabilities
+        const float inv_sl2 = 1.0f / a.sl2;
 
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    auto step = [&](uint32_t stage, int c0) {
-        int kbo = k_base + (int)stage;
-        uint32_t vb0 = v_base0 + vlds + stage, vb1 = v_base1 + vlds + stage;
-        asm volatile("" : "+v"(kbo), "+v"(vb0), "+v"(vb1));
-        // S^T = K Q^T: s[v] = S[row][key c0 + 8(v/4) + 4hf + v%4]
-        f32x16 s;
-        auto frag = [&](int x) { return *(const bf16x8*)(kst + (kbo ^ (x << 5))); };
-        bf16x8 kf[kBaRing];
+        // Fragment byte offsets: K rows `row` (+ 16), chunk grp (+ the k-step's); V by transposing
+        // reads, 16 lanes taking 4 keys x 16 elements.
+        const int k_base = row * ROWB | ((grp ^ tile_swz<D>(row)) << 4);
+        const int rl = 4 * grp + ((lane & 15) >> 2);
+        const int cl = (NR == 32 ? ((lane >> 4) & 1) * 2 : 0) + ((lane & 3) >> 1);
+        const int v_base0 = rl * ROWB | ((cl ^ tile_swz<D>(rl)) << 4) | ((lane & 1) << 3);
+        const int v_base1 = (rl + VSTEP) * ROWB | ((cl ^ tile_swz<D>(rl + VSTEP)) << 4) | ((lane & 1) << 3);
+        const char* kst = (const char*)tiles;
+        const uint32_t vlds = lds_addr(tiles) + ST * TK * ROWB;
+
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        auto step = [&](uint32_t stage, int c0) {
+            int kbo = k_base + (int)stage;
+            uint32_t vb0 = v_base0 + vlds + stage, vb1 = v_base1 + vlds + stage;
+            asm volatile("" : "+v"(kbo), "+v"(vb0), "+v"(vb1));
+            // S^T = K Q^T
+            Acc sa[KB];
+            constexpr int NX = KS * KB;                // fragment x: k-step x / KB, keys x % KB
+            auto frag = [&](int x) {
+                return *(const bf16x8*)(kst + (x % KB) * 16 * ROWB + (kbo ^ ((x / KB) * (2 * RB::kdim))));
+            };
+            bf16x8 kf[kBaRing];
 #pragma unroll
-        for (int i = 0; i < kBaRing; ++i) kf[i] = frag(i);
+            for (int i = 0; i < kBaRing; ++i) kf[i] = frag(i);
 #pragma unroll
-        for (int x = 0; x < KS; ++x) {
-            const bf16x8 cur = kf[x % kBaRing];
-            if (x + kBaRing < KS) kf[x % kBaRing] = frag(x + kBaRing);
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cur, qf[x], x == 0 ? f32x16{} : s, 0, 0, 0);
-        }
-        // V fragments, the first ones read ahead of the softmax: y = 2 db + k2
-        auto vfrag = [&](int y) {
-            const uint32_t rowo = (y & 1) * 16 * ROWB;
-            const v4i16 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_v4i16*)(uintptr_t)((vb0 ^ (y / 2 << 6)) + rowo));
-            const v4i16 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_v4i16*)(uintptr_t)((vb1 ^ (y / 2 << 6)) + rowo));
-            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
-        bf16x8 vf[kBaRingV];
+            for (int x = 0; x < NX; ++x) {
+                const bf16x8 cur = kf[x % kBaRing];
+                if (x + kBaRing < NX) kf[x % kBaRing] = frag(x + kBaRing);
+                sa[x % KB] = RB::mac(cur, qf[x / KB], x < KB ? Acc{} : sa[x % KB]);
+            }
+            // V fragments, the first ones read ahead of the softmax: y = PK db + k2
+            constexpr int NY = DB * PK;
+            auto vfrag = [&](int y) {
+                const uint32_t rowo = (y % PK) * 16 * ROWB;
+                const v4i16 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_v4i16*)(uintptr_t)((vb0 ^ (y / PK * (2 * NR))) + rowo));
+                const v4i16 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_v4i16*)(uintptr_t)((vb1 ^ (y / PK * (2 * NR))) + rowo));
+                return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+            };
+            bf16x8 vf[kBaRingV];
 #pragma unroll
-        for (int i = 0; i < kBaRingV; ++i) vf[i] = vfrag(i);
-        __builtin_amdgcn_sched_group_barrier(0x100, kBaRing, 0);
+            for (int i = 0; i < kBaRingV; ++i) vf[i] = vfrag(i);
+            __builtin_amdgcn_sched_group_barrier(0x100, kBaRing, 0);
 #pragma unroll
-        for (int x = 0; x < KS; ++x) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (x + kBaRing < KS) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            else __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        }
-        // The softmax before other waves' matrix products: the vector unit is the busier one (the
-        // reverse order, or none, takes 3-4% longer).
-        __builtin_amdgcn_s_setprio(1);
-        if (c0 + TK > open) {                          // the run's tail, or the causal future
-            const int e = lim4 - c0;
+            for (int x = 0; x < NX; ++x) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                if (x + kBaRing < NX) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                else __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            // The softmax before other waves' matrix products: the vector unit is the busier one (the
+            // reverse order, or none, takes 3-4% longer).
+            __builtin_amdgcn_s_setprio(1);
+            float s[NS];
 #pragma unroll
-            for (int v = 0; v < 16; ++v)
-                if (8 * (v >> 2) + (v & 3) > e) s[v] = -INFINITY;
-        }
-        float mk = fmaxf(s[0], s[1]), mk2 = fmaxf(s[2], s[3]);
+            for (int v = 0; v < NS; ++v) s[v] = sa[v / NV][v % NV];
+            if (c0 + TK > open) {                      // the run's tail, or the causal future
+                const int e = lim4 - c0;
 #pragma unroll
-        for (int v = 4; v < 16; v += 4) {
-            mk = fmaxf(fmaxf(mk, s[v]), s[v + 1]);
-            mk2 = fmaxf(fmaxf(mk2, s[v + 2]), s[v + 3]);
-        }
-        const float top = ba_pair_max(fmaxf(mk, mk2));
-        if (__any(top > thr)) {
-            const float mx = top * a.sl2;
-            const float m_new = mx > m_run + kBaSlack ? mx : m_run;
-            const float alpha = m_new == m_run ? 1.f : fast_exp2(m_run - m_new);
-            l0 *= alpha;
-            l1 *= alpha;
-            e0 *= alpha;
-            e1 *= alpha;
+                for (int v = 0; v < NS; ++v)
+                    if (VSTEP * (v >> 2) + (v & 3) > e) s[v] = -INFINITY;
+            }
+            float mk = fmaxf(s[0], s[1]), mk2 = fmaxf(s[2], s[3]);
 #pragma unroll
-            for (int db = 0; db < DB; ++db) o[db] *= alpha;
-            m_run = m_new;
-            // The maximum is rounded, the product in the multiply-add below is not: where
-            // logits are huge (a split of keys at the type's lowest value), what the rounding
-            // cut off would be an exponent of its own.  Such a row enters here for every tile, has
-            // the product rounded too and its logits moved to a maximum of 0.
-            const bool none = m_run == -INFINITY, huge = !none && fabsf(m_run) > kBaHuge;
-            m_ref = none || huge ? 0.f : m_run;          // (no visible key so far: exact zeros)
-            thr = huge ? -INFINITY : (m_run + kBaSlack) * inv_sl2;
-            if (__any(huge)) {
+            for (int v = 4; v < NS; v += 4) {
+                mk = fmaxf(fmaxf(mk, s[v]), s[v + 1]);
+                mk2 = fmaxf(fmaxf(mk2, s[v + 2]), s[v + 3]);
+            }
+            const float top = ba_group_max<NR>(fmaxf(mk, mk2));
+            if (__any(top > thr)) {
+                const float mx = top * a.sl2;
+                const float m_new = mx > m_run + kBaSlack ? mx : m_run;
+                const float alpha = m_new == m_run ? 1.f : fast_exp2(m_run - m_new);
+                l0 *= alpha;
+                l1 *= alpha;
+                e0 *= alpha;
+                e1 *= alpha;
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    float x = s[v] * a.sl2;
-                    asm volatile("" : "+v"(x));          // (not a multiply-add)
-                    s[v] = huge ? (x - m_run) * inv_sl2 : s[v];
+                for (int db = 0; db < DB; ++db) o[db] *= alpha;
+                m_run = m_new;
+                // The maximum is rounded, the product in the multiply-add below is not: where
+                // logits are huge (a split of keys at the type's lowest value), what the rounding
+                // cut off would be an exponent of its own.  Such a row enters here for every tile,
+                // has the product rounded too and its logits moved to a maximum of 0.
+                const bool none = m_run == -INFINITY, huge = !none && fabsf(m_run) > kBaHuge;
+                m_ref = none || huge ? 0.f : m_run;    // (no visible key so far: exact zeros)
+                thr = huge ? -INFINITY : (m_run + kBaSlack) * inv_sl2;
+                if (__any(huge)) {
+#pragma unroll
+                    for (int v = 0; v < NS; ++v) {
+                        float x = s[v] * a.sl2;
+                        asm volatile("" : "+v"(x));    // (not a multiply-add)
+                        s[v] = huge ? (x - m_run) * inv_sl2 : s[v];
+                    }
                 }
             }
-        }
-        bf16x8 pb[2];
+            bf16x8 pb[PK];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const float p = fast_exp2(fmaf(s[v], a.sl2, -m_ref));
-            (v & 1 ? e1 : e0) += p;
-            pb[v >> 3][v & 7] = (__bf16)p;
-        }
-        const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
+            for (int v = 0; v < NS; ++v) {
+                const float p = fast_exp2(fmaf(s[v], a.sl2, -m_ref));
+                (v & 1 ? e1 : e0) += p;
+                pb[v >> 3][v & 7] = (__bf16)p;
+            }
+            const bf16x2 one2 = {(__bf16)1.0f, (__bf16)1.0f};
 #pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2) {
-            const bf16x8 q8 = pb[k2];
-            l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 0, 1), one2, l0, false);
-            l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 2, 3), one2, l1, false);
-            l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 4, 5), one2, l0, false);
-            l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 6, 7), one2, l1, false);
-        }
-        __builtin_amdgcn_s_setprio(0);
-        // O^T += V^T P^T
+            for (int k2 = 0; k2 < PK; ++k2) {
+                const bf16x8 q8 = pb[k2];
+                l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 0, 1), one2, l0, false);
+                l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 2, 3), one2, l1, false);
+                l0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 4, 5), one2, l0, false);
+                l1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(q8, q8, 6, 7), one2, l1, false);
+            }
+            __builtin_amdgcn_s_setprio(0);
+            // O^T += V^T P^T
 #pragma unroll
-        for (int y = 0; y < 2 * DB; ++y) {
-            const bf16x8 cur = vf[y % kBaRingV];
-            if (y + kBaRingV < 2 * DB) vf[y % kBaRingV] = vfrag(y + kBaRingV);
-            o[y / 2] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cur, pb[y & 1], o[y / 2], 0, 0, 0);
+            for (int y = 0; y < NY; ++y) {
+                const bf16x8 cur = vf[y % kBaRingV];
+                if (y + kBaRingV < NY) vf[y % kBaRingV] = vfrag(y + kBaRingV);
+                o[y / PK] = RB::mac(cur, pb[y % PK], o[y / PK]);
+            }
+        };
+
+#pragma unroll
+        for (int tt = 0; tt < ST - 1; ++tt)
+            if (tt < ntile) issue(tt);
+        for (int tt = 0; tt < ntile; ++tt) {
+            // Tile tt has landed (the later one of the ring may be in flight), and every wave is
+            // done with the buffer that is filled next.
+            if (tt + 1 < ntile) wait_loads_barrier<LPW>();
+            else wait_loads_barrier<0>();
+            if (tt + ST - 1 < ntile) issue(tt + ST - 1);
+            if (live) step((uint32_t)(tt % ST) * (TK * ROWB), tt * TK);
+        }
+
+        // The partial rows: scaled by the largest finite element, transposed through LDS (the
+        // tiles are done with) and written as whole rows.
+        const float l_tot = ba_group_sum<NR>(l0 + l1), l_ex = ba_group_sum<NR>(e0 + e1);
+        asm volatile("" : "+v"(lane));
+        __syncthreads();
+        constexpr int OROW = 2 * D + 16;               // bytes of a row in LDS
+        static_assert(kBaRows * OROW <= (int)sizeof(tiles), "the rows fit the tiles");
+        char* orow = (char*)tiles + (w * NR) * OROW;
+        if (live) {
+            float top = 0.f;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const float x = fabsf(o[db][v]);
+                    top = x <= 3.4028235e38f ? fmaxf(top, x) : top;
+                }
+            top = ba_group_max<NR>(top);
+            const float inv = top > 0.f ? 1.0f / top : 1.f;
+            typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int j = 0; j < NV / 4; ++j)
+                    *(f16x4*)(orow + (lane & (NR - 1)) * OROW + 2 * (db * NR + 8 * j + 4 * (lane / NR))) =
+                        f16x4{(_Float16)(o[db][4 * j] * inv), (_Float16)(o[db][4 * j + 1] * inv),
+                              (_Float16)(o[db][4 * j + 2] * inv), (_Float16)(o[db][4 * j + 3] * inv)};
+            if (lane < n_val) a.part_s[part + lane] = float4{m_run, l_tot, l_ex, top > 0.f ? top : 1.f};
+            __builtin_amdgcn_wave_barrier();
+            _Float16* dst = a.part_o + part * D + lane * 8;
+#pragma unroll
+            for (int i = 0; i < NR / RPI; ++i) {
+                const int r = i * RPI + lane / CH;
+                const u32x4 v = *(const u32x4*)(orow + r * OROW + (lane % CH) * 16);
+                if (r < n_val) *(u32x4*)(dst + i * 512) = v;
+            }
         }
     };
-
-#pragma unroll
-    for (int tt = 0; tt < ST - 1; ++tt)
-        if (tt < ntile) issue(tt);
-    for (int tt = 0; tt < ntile; ++tt) {
-        // Tile tt has landed (the later one of the ring may be in flight), and every wave is done
-        // with the buffer that is filled next.
-        if (tt + 1 < ntile) wait_loads_barrier<LPW>();
-        else wait_loads_barrier<0>();
-        if (tt + ST - 1 < ntile) issue(tt + ST - 1);
-        if (live) step((uint32_t)(tt % ST) * (TK * ROWB), tt * TK);
-    }
-
-    // The partial rows: scaled by the largest finite element, transposed through LDS (the
-    // tiles are done with) and written as whole rows.
-    const float l_tot = ba_pair_sum(l0 + l1), l_ex = ba_pair_sum(e0 + e1);
-    asm volatile("" : "+v"(lane));
-    __syncthreads();
-    constexpr int OROW = 2 * D + 16;                     // bytes of a row in LDS
-    static_assert(kBaRows * OROW <= (int)sizeof(tiles), "the rows fit the tiles");
-    char* orow = (char*)tiles + (w * 32) * OROW;
-    if (live) {
-        float top = 0.f;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const float x = fabsf(o[db][v]);
-                top = x <= 3.4028235e38f ? fmaxf(top, x) : top;
-            }
-        top = ba_pair_max(top);
-        const float inv = top > 0.f ? 1.0f / top : 1.f;
-        typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                *(f16x4*)(orow + (lane & 31) * OROW + 2 * (db * 32 + 8 * j + 4 * (lane >> 5))) =
-                    f16x4{(_Float16)(o[db][4 * j] * inv), (_Float16)(o[db][4 * j + 1] * inv),
-                          (_Float16)(o[db][4 * j + 2] * inv), (_Float16)(o[db][4 * j + 3] * inv)};
-        if (lane < min(n_val, 32)) a.part_s[part + lane] = float4{m_run, l_tot, l_ex, top > 0.f ? top : 1.f};
-        __builtin_amdgcn_wave_barrier();
-        _Float16* dst = a.part_o + part * D + lane * 8;
-#pragma unroll
-        for (int i = 0; i < 32 / RPI; ++i) {
-            const int row = i * RPI + lane / CH;
-            const u32x4 v = *(const u32x4*)(orow + row * OROW + (lane % CH) * 16);
-            if (row < n_val) *(u32x4*)(dst + i * 512) = v;
-        }
-    }
+    if (small) run(Int<16>{});
+    else run(Int<32>{});
     if (!ctx || LIST || x >= x_end) return;
     __syncthreads();                                     // (the next item fills the tiles)
   }
@@ -765,8 +821,11 @@ BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_bat
     const long item_cap = (b.n_rows * G + kBaRows - 1) / kBaRows * p.H_kv;
     const long list_items = (long)b.n_rows * p.H_kv * ((G + kBaRows - 1) / kBaRows);
     const long suf_items = (long)b.tile_cap * p.H_kv;
-    w.ctx_wgs = n_sel == 0 ? kBaWgs : (int)(list_items > kBaWgs ? list_items : kBaWgs);
-    w.suf_wgs = (int)(suf_items > kBaWgs ? suf_items : kBaWgs);
+    auto wgs = [](long items) {
+        return (int)((items > kBaWgs ? items + kBaXcds - 1 : kBaWgs) / kBaXcds * kBaXcds);
+    };
+    w.ctx_wgs = n_sel == 0 ? kBaWgs : wgs(list_items);
+    w.suf_wgs = wgs(suf_items);
     w.suf_part = n_sel == 0 ? (kBaWgs + item_cap) * kBaRows : rows > least ? rows : least;
     const size_t parts = w.suf_part + (rows > least ? rows : least);
     w.part_s_off = (parts * p.d * 2 + 255) / 256 * 256;
@@ -868,6 +927,7 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
     a.nb = nb;
     a.tail = tail;
     a.ctx_wgs = w.ctx_wgs;
+    a.suf_wgs = w.suf_wgs;
     a.list_items = p.H_kv * ((G + kBaRows - 1) / kBaRows);
     a.list_tiles = (int)(((long)n_sel * block + kBaKeys - 1) / kBaKeys);
     a.sl2 = scale * kLog2e;
