@@ -499,6 +499,7 @@ relaxkv_status relaxkv_counts_to_host(const relaxkv_sets* s, int32_t* host_count
 #define RELAXKV_MAX_BATCH_ROWS 65536
 #define RELAXKV_MAX_BATCH_ROW_HEADS (1 << 22)      /* n_rows * H */
 #define RELAXKV_MAX_SELECTED_BLOCKS 2048
+#define RELAXKV_MAX_FRESH_ROWS (1 << 25)           /* rows of relaxkv_fresh_rows */
 
 /* Bit of a batch's error word counts[3]. */
 #define RELAXKV_BATCH_ERR_LENGTHS 1  /* a length below 0, past_b + new_b > max_suffix, or more
@@ -516,7 +517,8 @@ relaxkv_status relaxkv_counts_to_host(const relaxkv_sets* s, int32_t* host_count
  *   counts   [64]       rows of the step, row tiles, tokens of the longest suffix that a row
  *                       sees, error word; the rest is internal.
  * T_c, H, H_kv, d and dtype are those of the problem the batch was bound for; every call
- * refuses a batch of another shape.
+ * refuses a batch of another shape.  The arrays hold nothing until the first plan: in a buffer
+ * that is not zeroed, no other call may come before it.
  */
 typedef struct relaxkv_batch {
     int32_t n_seq, n_rows, max_suffix, tile_cap;

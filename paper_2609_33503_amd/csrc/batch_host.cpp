@@ -182,6 +182,7 @@ relaxkv_status relaxkv_fresh_rows(const relaxkv_problem* p, const relaxkv_rope* 
     if (st == RELAXKV_OK) st = rope_status(p, r, in);
     if (st != RELAXKV_OK) return st;
     if (!in->q != !q_out || !in->k != !k_out || !in->v != !v_out) return RELAXKV_EINVAL;
+    if (in->n_rows > RELAXKV_MAX_FRESH_ROWS) return RELAXKV_EUNSUPPORTED;
     if (!aligned(q_out) || !aligned(k_out) || !aligned(v_out)) return RELAXKV_EUNSUPPORTED;
     if (in->n_rows == 0 || (!in->q && !in->k && !in->v)) return RELAXKV_OK;
     if (!positions) return RELAXKV_EINVAL;

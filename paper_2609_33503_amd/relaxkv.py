@@ -276,6 +276,8 @@ def _cache_strides(t):
     """The layer, KV-head and token strides of a cache tensor for the descriptor
     (0, the dense value, for a dimension of size 1, whose stride torch leaves
     arbitrary and the library never uses)."""
+    if any(st == 0 and n > 1 for st, n in zip(t.stride()[:3], t.shape[:3])):
+        raise ValueError("an expanded tensor (stride 0) is no cache")
     return tuple(st if n > 1 else 0 for st, n in zip(t.stride()[:3], t.shape[:3]))
 
 
@@ -552,7 +554,7 @@ class Request:
                     and t.get_device() == self._index and t.stride(3) == 1):
                 _need_cache(t, name, self.dtype, shape, self.device)
         st = k.stride()
-        if st != v.stride() or batch.flat:                # (a dimension of size 1: any stride)
+        if st != v.stride() or batch.flat or 0 in st:     # (a dimension of size 1: any stride)
             st = _cache_strides(k)
             if st != _cache_strides(v):
                 raise ValueError("k_suffix and v_suffix must have the same strides")
@@ -565,13 +567,15 @@ class Request:
         if type(t) is _Tensor and t.dtype is self.dtype and t.is_cuda \
                 and t.get_device() == self._index and t.shape == (n, heads, self.d):
             st = t.stride()
-            if st[2] == 1 and st[1] == self.d and n > 1:
+            if st[2] == 1 and st[1] == self.d and n > 1 and st[0] > 0:
                 return st[0]
         if not isinstance(t, torch.Tensor) or t.device != self.device or t.dtype != self.dtype:
             raise ValueError(f"{name} must be a {self.dtype} tensor on {self.device}")
         _need_shape(t, name, (n, heads, self.d))
         if n and ((heads > 1 and t.stride(1) != self.d) or t.stride(2) != 1):
             raise ValueError(f"{name} must have contiguous rows")
+        if n > 1 and t.stride(0) == 0:
+            raise ValueError(f"{name} must not be expanded (row stride 0)")
         return t.stride(0) if n > 1 else 0
 
     def _rows(self, q, k, v, n):

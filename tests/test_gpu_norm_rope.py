@@ -156,3 +156,15 @@ def test_binding_refusals(gpu_lib):
         with pytest.raises(relaxkv.RelaxKVError):
             req.fresh_rows(**{**good, "rope": rope(d, rot, BF, True, False)})
     torch.cuda.synchronize()
+
+
+def test_expanded_rows_are_refused(gpu_lib):
+    """One row repeated by a stride of 0, which in the descriptor selects dense rows."""
+    req, r = request(4, 2, 64, BF), rope(64, 64, BF, True, False)
+    q = torch.zeros(1, 4, 64, dtype=BF, device="cuda").expand(5, 4, 64)
+    pos = torch.zeros(5, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        req.fresh_rows(r, pos, q, None, None, torch.zeros(5, 4, 64, dtype=BF, device="cuda"), None, None)
+    one = torch.ones(1, 4, 64, dtype=BF, device="cuda")
+    req.fresh_rows(r, pos[:1], one.expand(1, 4, 64), None, None, one, None, None)
+    torch.cuda.synchronize()

@@ -2,6 +2,7 @@
 No call here reaches a kernel: each is refused, or has no rows."""
 
 import ctypes
+import types
 
 import numpy as np
 import pytest
@@ -254,6 +255,31 @@ def test_rope_object_refusals(rk):
             rk.Rope(f)
     with pytest.raises(ValueError):
         rk.Rope(torch.zeros(8), q_weight=[1.0])
+
+
+def test_expanded_tensors_are_refused(rk):
+    """A stride of 0 selects the dense layout in the descriptors."""
+    for dim in range(3):
+        shape = [2, 3, 4, 64]
+        t = torch.zeros(shape)
+        assert rk._cache_strides(t) == (768, 256, 64)
+        with pytest.raises(ValueError):
+            rk._cache_strides(t.narrow(dim, 0, 1).expand(shape))
+    assert rk._cache_strides(torch.zeros(1, 3, 1, 64)) == (0, 64, 0)
+    req = types.SimpleNamespace(dtype=torch.float32, device=torch.device("cpu"), _index=-1, d=64)
+    rows = lambda t, n: rk.Request._projected(req, t, "q", 4, n)        # noqa: E731
+    fused = torch.zeros(5, 12, 64)
+    assert rows(fused[:, 4:8], 5) == 768 and rows(fused[:1, 4:8], 1) == 0 and rows(None, 5) == 0
+    with pytest.raises(ValueError):
+        rows(fused[:1, :4].expand(5, 4, 64), 5)
+    assert rows(fused[:1, :4].expand(1, 4, 64), 1) == 0
+
+
+def test_too_many_fresh_rows(rk):
+    p = _problem(rk)
+    b = _batch(rk, p)
+    a = _args(rk, p, b, rows=rk.CRows(0x4000, None, None, 0, 0, 0, (1 << 25) + 1), ko=None, vo=None)
+    assert _call(rk, "fresh_rows", a) == EUNSUPPORTED
 
 
 # ------------------------------------------------------------------ pins of the oracle
