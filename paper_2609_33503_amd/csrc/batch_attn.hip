@@ -18,13 +18,13 @@
 //   matrix products and waits overlap.  A wave owns 32 rows (16 where that covers the item;
 //   one row per lane): S^T = K Q^T, online softmax in the exp2 domain with a lazily raised
 //   maximum, O^T += V^T P^T.
-// - Probabilities are rounded to bf16 for the second product (2^-9 of each, independent over
+// - Probabilities are rounded to bf16 for the second product (2^-8 of each, independent over
 //   keys: about as much as rounding O once; float32 products would take eight times the matrix
 //   time).  The output is divided by the sum of the rounded ones, which keeps a row that
 //   sees one key exact, the log-sum-exp uses the sum of the exact ones.
 // - Every item writes its unnormalised output and (max, sums, scale); batch_merge adds them
 //   with weights exp2(max_s - max) in a fixed order.  The outputs are written as fp16 over
-//   the row's largest element (2^-12 of an element, an eighth of what rounding O to bf16 costs,
+//   the row's largest element (2^-11 of an element, an eighth of what rounding O to bf16 costs,
 //   for half the traffic of float32).
 // A row that sees no key gets O = 0 and lse = -inf.
 // Loads never leave a run's keys (past its end they repeat its last key, masked), so cache
@@ -35,6 +35,8 @@
 // log-sum-exps, which batch_merge_f32 adds in split order.
 
 #include <math.h>
+
+#include <algorithm>
 
 #include "attn_f32.h"
 #include "batch.h"
@@ -123,6 +125,13 @@ template <int NR> __device__ __forceinline__ float ba_group_max(float x) {
 }
 template <int NR> __device__ __forceinline__ float ba_group_sum(float x) {
     return RowBlock<NR>::groups(x, [](float a, float b) { return a + b; });
+}
+
+// Whether x is NaN, by its bits (this file is compiled for maxima and compares without NaN).
+__device__ __forceinline__ bool is_nan(float x) {
+    uint32_t u = __float_as_uint(x);
+    asm volatile("" : "+v"(u));
+    return (u & 0x7fffffffu) > 0x7f800000u;
 }
 
 // fill_lds16 with a wave-uniform base and a 32-bit byte offset per lane.
@@ -528,7 +537,10 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
                     *(f16x4*)(orow + (lane & (NR - 1)) * OROW + 2 * (db * NR + 8 * j + 4 * (lane / NR))) =
                         f16x4{(_Float16)(o[db][4 * j] * inv), (_Float16)(o[db][4 * j + 1] * inv),
                               (_Float16)(o[db][4 * j + 2] * inv), (_Float16)(o[db][4 * j + 3] * inv)};
-            if (lane < n_val) a.part_s[part + lane] = float4{m_run, l_tot, l_ex, top > 0.f ? top : 1.f};
+            // (a NaN sum under a maximum of -inf, where no logit is a number, must not pass for a
+            // split without keys)
+            if (lane < n_val)
+                a.part_s[part + lane] = float4{is_nan(l_ex) ? 0.f : m_run, l_tot, l_ex, top > 0.f ? top : 1.f};
             __builtin_amdgcn_wave_barrier();
             _Float16* dst = a.part_o + part * D + lane * 8;
 #pragma unroll
@@ -699,7 +711,7 @@ __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a
     const BatchSplit sp = load_split(a.counts);
     int n_split, kps;
     f32_split<LIST>(a, sp, n_split, kps);
-    int x = blockIdx.x;
+    int x = (int)(blockIdx.y * gridDim.x + blockIdx.x);
     const int split = x % n_split;
     x /= n_split;
     const int g = x % a.Hkv;
@@ -769,7 +781,10 @@ __global__ __launch_bounds__(256) void batch_merge_f32(BaF32Args a) {
     const long rows = (long)sp.rows * a.H;
     if (n == 1 || th >= rows) return;
     float M = -INFINITY;
-    for (int s = lane; s < n; s += 64) M = fmaxf(M, a.part_l[s * rows + th]);
+    for (int s = lane; s < n; s += 64) {
+        const float l = a.part_l[s * rows + th];
+        M = fmaxf(M, is_nan(l) ? 0.f : l);               // (not a row without keys)
+    }
     M = wave_max(M);
     const float ref = M == -INFINITY ? 0.f : M;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -883,7 +898,9 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
         auto go = [&](auto d_t, auto list_t) {
             constexpr int D = decltype(d_t)::value;
             constexpr bool LIST = decltype(list_t)::value;
-            hipLaunchKernelGGL((battn_f32<D, LIST>), dim3(w.ctx_wgs), dim3(MfmaF32<16>::waves * 64),
+            // (a launch dimension holds fewer than 2^32 threads)
+            const unsigned nx = std::min(w.ctx_wgs, 1 << 20);
+            hipLaunchKernelGGL((battn_f32<D, LIST>), dim3(nx, (w.ctx_wgs + nx - 1) / nx), dim3(MfmaF32<16>::waves * 64),
                                sizeof(AttnF32Lds<D, kBatchRowsF32>) + (LIST ? (n_sel + 2) * sizeof(int) : 0),
                                st, a);
             hipLaunchKernelGGL((batch_merge_f32<D, LIST>), dim3((unsigned)(((long)b.n_rows * p.H + 3) / 4)),

@@ -15,15 +15,15 @@ def attn_tol(O, spread, sharp=1.0):
       normaliser take the same rounded values, so O moves by at most 2^-8 spread.  (Two keys of
       equal weight rounded opposite ways reach it.)
     - O is rounded once: 2^-8 |O|.
-    - The partial outputs of the key splits are rounded to fp16, 2^-12 of each: with weights
-      that sum to one, at most 2^-12 sum_j p_j |V_j| <= 2^-12 (spread + |O|).
+    - The partial outputs of the key splits are rounded to fp16, half a step of 11 bits, 2^-11 of
+      each: with weights that sum to one, at most 2^-11 sum_j p_j |V_j| <= 2^-11 (spread + |O|).
     - Float32 logits: 130 roundings (128 products, the scale, the maximum) of 2^-24 of a sum
       of |q_c k_c| / sqrt(d), about 0.64 d / sqrt(d) = 7.2 for normal q and k at d 128 and
       below 13 for all of them: 1e-4, times `sharp` where the queries are scaled by it.  Each p
       is off by that factor, O by that much of the spread.
     - 1% for the products of these, 1e-6 for what is near zero."""
     h = HALF[torch.bfloat16]
-    return 1.01 * h * (1 + 2.0 ** -4) * (spread + np.abs(O)) + 1e-4 * sharp * spread + 1e-6
+    return 1.01 * h * (1 + 2.0 ** -3) * (spread + np.abs(O)) + 1e-4 * sharp * spread + 1e-6
 
 
 def f64(t):

@@ -176,6 +176,74 @@ def test_lowest_keys(gpu_lib, low):
     s.check(ref)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("T,block", [(640, None), (640, 64), (20, None), (9000, None)])
+def test_not_finite_reaches_the_rows_that_see_it(gpu_lib, T, block, dtype):
+    """A NaN in a query or a key that a row sees, or a logit of +inf: its output and its
+    log-sum-exp are NaN, also where none of its logits is a number, and only its own."""
+    s = Step(past=[20, 3, 9], new=[1, 3, 1], T=T, seed=9, dtype=dtype)
+    s.q[4, :, 1] = 1.0
+    lists = None
+    if block:
+        lists = torch.arange(T // block, dtype=torch.int32, device="cuda").expand(5, 2, -1).contiguous()
+    O, lse, spread = s.reference(lists, block)
+    s.q[0, 2, 5] = float("nan")
+    s.ks[1, :, 4, 7] = float("nan")                   # the second new token of request 1
+    s.ks[2, 0, 9, 1] = float("inf")
+    bad = np.zeros((5, 8), bool)
+    bad[0, 2] = bad[2:4] = bad[4, :4] = True
+    if block:
+        s.blocks(block, lists)
+    else:
+        s.shared()
+    assert np.array_equal(np.isnan(f64(s.lse)), bad)
+    assert np.array_equal(np.isnan(f64(s.out)), np.broadcast_to(bad[..., None], O.shape))
+    at = torch.from_numpy(bad).cuda()
+    s.out[at], s.lse[at] = torch.from_numpy(O[bad]).to(s.out), torch.from_numpy(lse[bad]).to(s.lse)
+    s.check((O, lse, spread))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_largest_step(gpu_lib, dtype):
+    """The most rows, heads and requests of a step: one new token each over one context key
+    and its own, softmax of two logits."""
+    n, H, d = 65536, 64, 64
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of device memory")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rnd = lambda *sh: torch.randn(*sh, device="cuda", generator=g).to(dtype)    # noqa: E731
+    kc, vc, ks, vs = rnd(1, H, 1, d), rnd(1, H, 1, d), rnd(n, H, 1, d), rnd(n, H, 1, d)
+    q = rnd(n, H, d)
+    req = relaxkv.Request(torch.zeros(1, 1, H, d, dtype=dtype, device="cuda"), kc, vc, 0.5)
+    b = req.alloc_batch(n, n, 1)
+    z = torch.zeros(n, dtype=torch.int32, device="cuda")
+    req.plan_batch(b, z, z + 1)
+    assert b.counts_to_host() == [n, n, 1, 0]
+    out = torch.empty_like(q)
+    lists = torch.zeros(n, H, 1, dtype=torch.int32, device="cuda")
+    for blocks in (False, True):
+        out.zero_()
+        if blocks:
+            ws = req.alloc_block_workspace(b, 16, 1)
+            req.block_attn(b, 0, kc, vc, 16, lists, q, ks, vs, out, None, ws)
+        else:
+            ws = req.alloc_shared_workspace(b)
+            req.shared_attn(b, 0, kc, vc, q, ks, vs, out, None, ws)
+        del ws
+        for i in range(0, n, 8192):
+            Q, K, V = (t[i:i + 8192].double().reshape(-1, H, d) for t in (q, ks, vs))
+            K0, V0 = kc[0, :, 0].double(), vc[0, :, 0].double()
+            p = torch.sigmoid(((Q * K).sum(-1) - (Q * K0).sum(-1)) * d ** -0.5)[..., None]
+            O = p * V + (1 - p) * V0
+            spread = p * (V - O).abs() + (1 - p) * (V0 - O).abs()
+            err = (out[i:i + 8192].double() - O).abs()
+            if dtype == BF:                           # attn_tol
+                tol = 1.01 * 2.0 ** -8 * (1 + 2.0 ** -3) * (spread + O.abs()) + 1e-4 * spread + 1e-6
+            else:
+                tol = torch.full_like(O, 1e-5 * float(O.abs().max()))
+            assert bool((err <= tol).all())
+
+
 def test_bit_identical_runs_and_streams(gpu_lib):
     """Same bits on every run, on another stream and with a used workspace."""
     s = Step(past=[100, 3, 60], new=[1, 20, 1], T=3000, H=16, H_kv=4)
@@ -246,4 +314,18 @@ def test_binding_refusals(gpu_lib):
     for bad in (dict(block=48), dict(blocks=torch.zeros(3, 2, 5, dtype=torch.int32, device="cuda"))):
         with pytest.raises(relaxkv.RelaxKVError):
             s.req.block_attn(**{**blk, **bad})
+    torch.cuda.synchronize()
+
+
+def test_expanded_suffix_is_refused(gpu_lib):
+    """A stride of 0 (an expanded tensor) selects the dense layout in the descriptor, so it must
+    not get there."""
+    s = Step(past=[5, 1], new=[2, 1], T=200)
+    ws = s.req.alloc_shared_workspace(s.batch)
+    for dim in range(3):
+        k = s.ks.narrow(dim, 0, 1).expand(s.ks.shape)
+        with pytest.raises(ValueError):
+            s.req.shared_attn(s.batch, 0, s.kc, s.vc, s.q, k, k, s.out, s.lse, ws)
+        with pytest.raises(ValueError):
+            s.req.batch_rows(relaxkv.Rope(), s.batch, None, None, None, None, k, k)
     torch.cuda.synchronize()
