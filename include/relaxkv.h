@@ -633,6 +633,7 @@ size_t relaxkv_shared_attn_workspace_bytes(const relaxkv_problem* p, const relax
  *   suffix    the layer's suffix caches, which already hold the step's new tokens.
  *   out       device out [n_rows][H][d] in dtype; lse_out optional [n_rows][H] float32, the
  *             natural-log normaliser.  Rows behind the step's last are left as they are.
+ *             out may be q.
  *   ws        device scratch of ws_bytes >= relaxkv_shared_attn_workspace_bytes(p, b); two
  *             calls that share it must be ordered.
  * The same call gives the same bits on every run.  The last bits of a row depend on the

@@ -6,7 +6,7 @@ import numpy as np
 import pytest
 import torch
 
-from batch_harness import Step, f64
+from batch_harness import Step, attn_tol, f64
 from paper_2609_33503_amd import relaxkv
 
 pytestmark = pytest.mark.gpu
@@ -315,6 +315,72 @@ def test_binding_refusals(gpu_lib):
         with pytest.raises(relaxkv.RelaxKVError):
             s.req.block_attn(**{**blk, **bad})
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_output_in_place_of_the_queries(gpu_lib, dtype):
+    for kw in (SHARED["mixed"], SHARED["suffix-splits"], SHARED["one"]):
+        s = Step(dtype=dtype, **kw)
+        s.shared()
+        want, x = s.out.clone(), s.q.clone()
+        ws = s.req.alloc_shared_workspace(s.batch)
+        s.req.shared_attn(s.batch, 0, s.kc, s.vc, x, s.ks, s.vs, x, None, ws)
+        assert torch.equal(x[:s.n], want[:s.n])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_offsets_past_32_bits(gpu_lib, dtype):
+    """The last layer and head of a cache of more than 2^32 elements, and suffixes 2^31 elements apart,
+    written by batch_rows: against a short cache of the same keys."""
+    L, H, T, d = 6, 16, 1 << 19, 128
+    if torch.cuda.mem_get_info()[0] < 110 << 30:
+        pytest.skip("needs 110 GB of device memory")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *sh: torch.randn(*sh, device="cuda", generator=g).to(dtype)    # noqa: E731
+    far, n, block, m = 1 << 31, 3, 64, 20
+    kc, vc = (torch.zeros(L, H, T, d, dtype=dtype, device="cuda") for _ in range(2))
+    kc[-1, :, -m * block:], vc[-1, :, -m * block:] = rnd(H, m * block, d), rnd(H, m * block, d)
+    buf = [torch.zeros(far * (n - 1) + H * 2 * d, dtype=dtype, device="cuda") for _ in range(2)]
+    ks, vs = (b.as_strided((n, H, 2, d), (far, 2 * d, d, 1)) for b in buf)
+    req = relaxkv.Request(torch.zeros(L, 1, H, d, dtype=dtype, device="cuda"), kc, vc, 0.5)
+    b = req.alloc_batch(n, n, 2)
+    z = torch.zeros(n, dtype=torch.int32, device="cuda")
+    req.plan_batch(b, z, z + 1)
+    q, k, v = rnd(n, H, d), rnd(n, H, d), rnd(n, H, d)
+    qr, out = torch.empty_like(q), torch.empty_like(q)
+    req.batch_rows(relaxkv.Rope(), b, q, k, v, qr, ks, vs)
+    assert torch.equal(qr, q) and torch.equal(ks[:, :, 0], k) and torch.equal(vs[:, :, 0], v)
+    nb = T // block
+    lists = torch.arange(nb - m, nb, dtype=torch.int32, device="cuda").expand(n, H, m).contiguous()
+    req.block_attn(b, L - 1, kc, vc, block, lists, q, ks, vs, out, None, req.alloc_block_workspace(b, block, m))
+    sk, sv = (t[-1:, :, -m * block:].contiguous() for t in (kc, vc))
+    short = relaxkv.Request(torch.zeros(1, 1, H, d, dtype=dtype, device="cuda"), sk, sv, 0.5)
+    c = short.alloc_batch(n, n, 2)
+    short.plan_batch(c, z, z + 1)
+    want, dense = torch.empty_like(q), [t.contiguous() for t in (ks, vs)]
+    short.block_attn(c, 0, sk, sv, block, lists - (nb - m), q, *dense, want, None,
+                     short.alloc_block_workspace(c, block, m))
+    assert torch.equal(out, want) and bool(want.any(-1).all())
+    # All of the cache: the other keys are 0, and so are their values.
+    lse = torch.empty(n, H, device="cuda")
+    req.shared_attn(b, L - 1, kc, vc, q, ks, vs, out, lse, req.alloc_shared_workspace(b))
+    zeros = T - m * block
+    K, V = (torch.cat((t[0].double().expand(n, -1, -1, -1), o[:, :, None].double()), 2)
+            for t, o in ((sk, k), (sv, v)))
+    x = (K * q[:, :, None].double()).sum(-1) * d ** -0.5
+    z = x.exp().sum(-1) + zeros
+    p = (x.exp() / z[..., None])[..., None]
+    O = (p * V).sum(2)
+    spread = (p * (V - O[:, :, None]).abs()).sum(2) + (zeros / z)[..., None] * O.abs()
+    O, spread = f64(O), f64(spread)
+    tol = attn_tol(O, spread) if dtype == BF else 1e-5 * np.abs(O).max()
+    assert np.all(np.abs(f64(out) - O) <= tol)
+    assert np.abs(f64(lse) - f64(z.log())).max() <= 5e-4
+    mean = torch.empty(L, H, nb, d, dtype=dtype, device="cuda")
+    req.block_means(None, kc, block, mean)
+    one = torch.empty(1, H, m, d, dtype=dtype, device="cuda")
+    short.block_means(0, sk, block, one)
+    assert torch.equal(mean[-1, :, -m:], one[0]) and not mean[:-1].any() and not mean[-1, :, :-m].any()
 
 
 def test_expanded_suffix_is_refused(gpu_lib):
