@@ -95,8 +95,11 @@ __device__ __forceinline__ void list_split(const BaArgs& a, int rows, int& n, in
 }
 
 // MFMA blocks of NR (token, head) rows: the lane's row is lane % NR, its group lane / NR.
-// Value v of a 32-key tile's logits is key key0(v) + 4 group, value v of an output block is element
+// Value v of a 32-key tile's logits is key key0(v) + 4 kg, value v of an output block is element
 // key0(v) + 4 group of the block's NR ones (key0: 8 (v/4) + v%4 for 32 rows, 16 (v/4) + v%4 for 16).
+// kg is the group; for 16 rows the middle two of the four change places (the K rows that are fed
+// to the product do), so that the V rows that 32 lanes read, 0 - 3 and 8 - 11, lie in different
+// banks under the tiles' swizzle.
 template <int NR> struct RowBlock;
 template <> struct RowBlock<32> {
     typedef f32x16 Acc;
@@ -358,7 +361,9 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
         constexpr int DB = D / NR, PK = 32 / RB::kdim; // d blocks of O^T, products of each per tile
         constexpr int VSTEP = NR == 32 ? 8 : 16;       // keys between a lane's runs of four
         const int row = lane & (NR - 1), grp = lane / NR;
-        const int lim4 = lim - 4 * grp;
+        const int kg = NR == 16 ? grp >> 1 | (grp & 1) << 1 : grp;
+        const int krow = NR == 16 ? (row & 3) | (row & 4) << 1 | (row & 8) >> 1 : row;
+        const int lim4 = lim - 4 * kg;
         bf16x8 qf[KS];
         {
             const uint16_t* qrow = a.q + ((size_t)t * a.H + g * a.G + hh) * D;
@@ -376,10 +381,10 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
         float l0 = 0.f, l1 = 0.f, e0 = 0.f, e1 = 0.f;  // sums of rounded and exact probabilities
         const float inv_sl2 = 1.0f / a.sl2;
 
-        // Fragment byte offsets: K rows `row` (+ 16), chunk grp (+ the k-step's); V by transposing
+        // Fragment byte offsets: K rows `krow` (+ 16), chunk grp (+ the k-step's); V by transposing
         // reads, 16 lanes taking 4 keys x 16 elements.
-        const int k_base = row * ROWB | ((grp ^ tile_swz<D>(row)) << 4);
-        const int rl = 4 * grp + ((lane & 15) >> 2);
+        const int k_base = krow * ROWB | ((grp ^ tile_swz<D>(krow)) << 4);
+        const int rl = 4 * kg + ((lane & 15) >> 2);
         const int cl = (NR == 32 ? ((lane >> 4) & 1) * 2 : 0) + ((lane & 3) >> 1);
         const int v_base0 = rl * ROWB | ((cl ^ tile_swz<D>(rl)) << 4) | ((lane & 1) << 3);
         const int v_base1 = (rl + VSTEP) * ROWB | ((cl ^ tile_swz<D>(rl + VSTEP)) << 4) | ((lane & 1) << 3);
