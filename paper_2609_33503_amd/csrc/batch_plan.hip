@@ -8,7 +8,7 @@
 // which empties the whole plan), scans its own requests in LDS, and its threads take its rows
 // one each, finding their request by binary search in that scan, so that one request of
 // many rows is spread over the workgroup as many requests of one row are.
-// 61 rows of 64 requests 8.5 us per call back to back, 27376 rows of 1500 requests 9.0 us.
+// 61 rows of 64 requests 5.6 us per call back to back, 27376 rows of 1500 requests 6.7 us.
 
 #include "batch.h"
 #include "dev_common.h"

