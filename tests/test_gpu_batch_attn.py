@@ -244,6 +244,62 @@ def test_largest_step(gpu_lib, dtype):
             assert bool((err <= tol).all())
 
 
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,H_kv,past,new,T", [
+    (160, 1, [3, 70], [2, 1], 300),           # a group's second chunk of 32 heads
+    (129, 1, [3], [1], 100),                  # of one head
+    (8, 2, [5] * 33, [1] * 33, 700),          # 132 rows: a last chunk of 4
+    (8, 2, [5] * 33, [1] * 33, 8000),
+    (8, 2, [0] * 7, [7] * 7, 100),            # 196 rows: of 68
+    (10, 10, [2, 9, 0], [1, 1, 17], 520),     # heads that do not divide over the XCDs
+    (65, 1, [30], [1], 64), (64, 1, [30], [1], 65),     # around the rows that 16-row waves hold
+])
+def test_chunk_borders(gpu_lib, H, H_kv, past, new, T, d, dtype):
+    s = Step(past=past, new=new, T=T, H=H, H_kv=H_kv, d=d, dtype=dtype, seed=12, room=max(
+        p + n for p, n in zip(past, new)))
+    s.shared()
+    s.check(s.reference(), "shared")
+    nb = -(-T // 32)
+    lists = torch.from_numpy(_lists(np.random.default_rng(1), s.n, H_kv, nb, min(nb, 11))).cuda()
+    s.out.fill_(7.0), s.lse.fill_(7.0)
+    s.blocks(32, lists)
+    s.check(s.reference(lists, 32), "blocks")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_smallest_and_largest_scales(gpu_lib, dtype):
+    """Under a tiny scale all keys weigh the same; under a huge one the largest logit alone counts:
+    the next one is further below it than a float32 logit is rounded."""
+    for scale in (1e-30, 1e-37):
+        s = Step(past=[30, 2], new=[1, 2], T=300, seed=6, dtype=dtype, scale=scale)
+        s.shared()
+        s.check(s.reference())
+    for scale in (1e5, 1e30):
+        for T in (300, 5000):
+            s = Step(past=[30, 2], new=[1, 2], T=T, seed=6, dtype=dtype, scale=scale)
+            s.shared()
+            q, k, v = f64(s.q), f64(s.kc[0]), f64(s.vc[0])
+            seen = 0
+            for t in range(s.n):
+                own = slice(0, int(s.pos[t]) - T + 1)
+                for h in range(s.H):
+                    g = h // (s.H // s.H_kv)
+                    K, V = (np.concatenate((c[g], f64(x[s.seq[t], g, own]))) for c, x in ((k, s.ks), (v, s.vs)))
+                    x = K @ q[t, h]
+                    i, j = np.argsort(-x)[:2]
+                    # Each logit is off by 130 roundings of 2^-24 of the sum of its products' sizes;
+                    # where the two are closer than that, either may win.
+                    err = 2 * 130 * 2.0 ** -24 * (np.abs(K[[i, j]]) @ np.abs(q[t, h])).max()
+                    if (x[i] - x[j] - err) * scale < 30:
+                        continue
+                    seen += 1
+                    got = f64(s.out[t, h])
+                    assert np.all(np.abs(got - V[i]) <= 1e-6 + 2.0 ** -20 * np.abs(V).max()), (scale, T, t, h)
+                    assert abs(float(s.lse[t, h]) - x[i] * scale) <= err * scale + 1
+            assert seen >= s.n * s.H // 2
+
+
 def test_bit_identical_runs_and_streams(gpu_lib):
     """Same bits on every run, on another stream and with a used workspace."""
     s = Step(past=[100, 3, 60], new=[1, 20, 1], T=3000, H=16, H_kv=4)
