@@ -33,6 +33,7 @@ struct alignas(16) BatchTile {
 constexpr int kBaRows = kBatchRowsBf16;
 constexpr int kBaKeys = 32;            // keys per tile
 constexpr int kBaWgs = 768;            // workgroups the splits aim for (three per CU)
+constexpr int kBaItemWgs = 512;        // of them for context items that one worker has alone
 constexpr int kBaMinTiles = 8;         // fewest tiles per split
 constexpr int kBaXcds = 8;
 constexpr int kBaLongSuffix = 1024;    // tokens from which the suffix items go first
@@ -78,8 +79,11 @@ __host__ __device__ inline BatchSplit batch_split(int rows, int row_tiles, int l
     s.tiles = (T + kBaKeys - 1) / kBaKeys;
     const int most = (s.tiles + kBaMinTiles - 1) / kBaMinTiles;
     // One chunk of rows is bound by memory, and one workgroup per CU streams better than three
-    // with a third of the keys (1-16 requests over 32K: 34-40 us, 38-44).
-    const int wgs = s.chunks == 1 ? kBaWgs / 3 : kBaWgs;
+    // with a third of the keys (1-16 requests over 32K: 34-40 us, 38-44).  Several chunks take
+    // two per CU and leave the third place to the suffix items, which then run beside them (with
+    // suffixes of 300 tokens: 160 rows over 32K 52 us, 56 with three; 384 rows 80, 88; 640 rows 131,
+    // 145; 320 rows over 8K 40, 46; without suffixes 320 rows over 32K 67, 68).
+    const int wgs = s.chunks == 1 ? kBaWgs / 3 : kBaItemWgs;
     int n = s.items > 0 ? wgs / s.items : 0;
     n = n < most ? n : most;
     // (whole rounds of the XCDs)
@@ -97,8 +101,9 @@ __host__ __device__ inline BatchSplit batch_split(int rows, int row_tiles, int l
         s.workers = (int32_t)((all + s.quota - 1) / s.quota);
     }
     // Long suffixes are bound by memory, several chunks of rows by computation: the suffix items
-    // go first, so that the two overlap (64 requests of 1500 suffix tokens over 32K: 131 us, 150
-    // with them last); short ones go last, behind the longer items (600 tokens: 72, 75 first).
+    // go first, so that the two overlap (64 requests of 5 rows with 3000 suffix tokens over 32K: 189
+    // us, 210 with them last; 128 of 4 rows with 1500 over 8K: 155, 168); short ones go last,
+    // behind the longer items (64 with up to 700 over 32K: 68, 72 first).
     s.suffix_first = s.chunks > 1 && longest >= kBaLongSuffix;
     int quota;
     batch_split_keys((longest + kBaKeys - 1) / kBaKeys, row_tiles * Hkv, kBaWgs, kBaMinTiles, s.suf_n,
