@@ -26,10 +26,11 @@
 //   with weights exp2(max_s - max) in a fixed order.  The outputs are written as fp16 over
 //   the row's largest element (2^-11 of an element, an eighth of what rounding O to bf16 costs,
 //   for half the traffic of float32).
-// 64 decoding requests of 40/8 heads over 32K keys, d 128: 69 us and 9 of merge (its K and V once and
-// the suffixes: 37 us at 6.07 TB/s); 20 questions of 761 tokens in all, 32/8 heads, over 8K: 115 and
-// 13 (85 at 1188 TFLOP/s).  While it runs MFMA and vector unit are busy 28-42% and 38-48%, rarely
-// together; neither memory (fills alone take 22 and 43 us) nor LDS (22%) bounds it.
+// 64 decoding requests of 40/8 heads over 32K keys, d 128: 63 us and 7.3 of merge (its K and V once and
+// the suffixes: 37 us at 6.07 TB/s); 20 questions of 761 tokens in all, 32/8 heads, over 8K: 116 and
+// 13 (85 at 1188 TFLOP/s).  While it runs MFMA and vector unit are busy 30-42% and 39-48%, rarely
+// together, LDS 23%.  384 rows per KV head take 49-53 us more for 32K more keys, and as much without
+// the fills, which alone take 33: the arithmetic at the clock that the power limit leaves.
 // A row that sees no key gets O = 0 and lse = -inf.
 // Loads never leave a run's keys (past its end they repeat its last key, masked), so cache
 // rows past the context and suffix tokens past a request's length are never read.
