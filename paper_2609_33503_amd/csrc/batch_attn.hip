@@ -76,7 +76,7 @@ struct BaArgs {
     _Float16* part_o;
     float4* part_s;          // (max, sum of rounded, sum of exact probabilities, scale)
     size_t suf_part;
-    int T, H, Hkv, G, n_rows, n_sel, bshift, nb, tail;
+    int T, H, Hkv, G, n_sel, bshift, nb, tail;
     int ctx_wgs, suf_wgs;    // workgroups of the launch for context and suffix items
     int list_tiles, list_items;   // listed: key tiles of a row at most, items of a token
     float sl2;               // softmax scale * log2(e)
@@ -692,7 +692,7 @@ struct BaF32Args {
     int64_t c_sh, c_st, s_ss, s_sh, s_st;
     const int32_t *counts, *row_seq, *row_pos, *lists;
     const BatchTile* tiles;
-    int T, H, Hkv, G, n_rows, n_sel, bshift, nb, tail;
+    int T, H, Hkv, G, n_sel, bshift, nb, tail;
     int list_tiles, list_items;      // listed: kBaF32Keys of a row at most (and its suffix), items
     float scale;
     float *out, *lse;
@@ -892,7 +892,6 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
         a.H = p.H;
         a.Hkv = p.H_kv;
         a.G = G;
-        a.n_rows = b.n_rows;
         a.n_sel = n_sel;
         a.bshift = bshift;
         a.nb = nb;
@@ -948,7 +947,6 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
     a.H = p.H;
     a.Hkv = p.H_kv;
     a.G = G;
-    a.n_rows = b.n_rows;
     a.n_sel = n_sel;
     a.bshift = bshift;
     a.nb = nb;
