@@ -37,9 +37,11 @@ constexpr int kBaItemWgs = 512;        // of them for context items that one wor
 constexpr int kBaMinTiles = 8;         // fewest tiles per split
 constexpr int kBaXcds = 8;
 constexpr int kBaLongSuffix = 1024;    // tokens from which the suffix items go first
-// float32: a split's keys are at least one block for each of the 16 waves, its workgroups one
-// round (one per CU at d 128).
-constexpr int kBaF32Keys = 256, kBaF32Wgs = 256;
+// float32: a split's keys are at least one block for each of the 16 waves; one workgroup per CU
+// (at d 128); up to kBaF32More splits more where as many as kBaF32Items items leave CUs of the
+// last round idle (64 requests of 5 rows, 8 heads, over 8K: 157 us, 197 without; over 32K 543, 778).
+constexpr int kBaF32Keys = 256, kBaF32Wgs = 256, kBaF32Items = 512, kBaF32More = 3;
+constexpr int kBaF32Parts = kBaF32Wgs + kBaF32More * kBaF32Items;     // workgroups of several splits
 constexpr int kBatchSplitAt = 16;      // first word of the split in relaxkv_batch::counts
 
 // Shared context: item (g, chunk) = g * chunks + chunk holds `tiles` key tiles, worker w takes
@@ -56,7 +58,8 @@ struct BatchSplit {
     int32_t per_item;                  // workers of an item; 0: cut anywhere
     int32_t suffix_first;              // order of the items in the launch
     int32_t suf_n, suf_kps;            // suffix splits, keys each
-    int32_t f32_n, f32_kps;            // float32: splits of a row tile's keys, keys each
+    int32_t f32_n, f32_kps;            // float32: splits of the context, keys each
+    int32_t f32_sn, f32_skps;          // and of a row tile's suffix
 };
 
 // Splits n of `tiles` key tiles, `quota` (at least `least`) tiles each, so that `items` of them
@@ -109,9 +112,25 @@ __host__ __device__ inline BatchSplit batch_split(int rows, int row_tiles, int l
     batch_split_keys((longest + kBaKeys - 1) / kBaKeys, row_tiles * Hkv, kBaWgs, kBaMinTiles, s.suf_n,
                      quota);
     s.suf_kps = quota * kBaKeys;
-    batch_split_keys((T + longest + kBaF32Keys - 1) / kBaF32Keys, row_tiles * Hkv, kBaF32Wgs, 1, s.f32_n,
-                     s.f32_kps);
-    s.f32_kps *= kBaF32Keys;
+    // A workgroup takes about as long as its units of kBaF32Keys keys and one more.
+    auto f32_split = [&](int keys, int items, int& n, int& kps) {
+        const int units = (keys + kBaF32Keys - 1) / kBaF32Keys;
+        batch_split_keys(units, items, kBaF32Wgs, 1, n, kps);
+        const int least = n, more = items <= kBaF32Items ? kBaF32More : 0;
+        int best = (n * items + kBaF32Wgs - 1) / kBaF32Wgs * (kps + 1);
+        for (int i = least + 1; i <= least + more && i <= units; ++i) {
+            const int quota = (units + i - 1) / i, m = (units + quota - 1) / quota;
+            const int cost = (m * items + kBaF32Wgs - 1) / kBaF32Wgs * (quota + 1);
+            if (cost < best) {
+                best = cost;
+                n = m;
+                kps = quota;
+            }
+        }
+        kps *= kBaF32Keys;
+    };
+    f32_split(T, (rows * G + kBatchRowsF32 - 1) / kBatchRowsF32 * Hkv, s.f32_n, s.f32_kps);
+    f32_split(longest, row_tiles * Hkv, s.f32_sn, s.f32_skps);
     return s;
 }
 
@@ -125,7 +144,8 @@ struct BatchAttnWorkspace {
 };
 
 // n_sel = 0: the whole context.
-BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_batch& b, int n_sel);
+BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_batch& b, int block,
+                                     int n_sel);
 size_t block_select_bytes(const relaxkv_problem& p, const relaxkv_batch& b, int block);
 
 inline int block_count(const relaxkv_problem& p, int block) { return (p.T_c + block - 1) / block; }

@@ -35,9 +35,11 @@
 // Loads never leave a run's keys (past its end they repeat its last key, masked), so cache
 // rows past the context and suffix tokens past a request's length are never read.
 //
-// float32: the MFMA core of attn_f32.h, 16 rows of one request per workgroup over one split of
-// their context and suffix keys; with more than one split they write normalised outputs and
-// log-sum-exps, which batch_merge_f32 adds in split order.
+// float32: the MFMA core of attn_f32.h over the same two kinds of items, 16 rows each: rows of all
+// requests over a split of the context, rows of one request over a split of its suffix.  Each
+// writes normalised outputs and log-sum-exps, which batch_merge_f32 adds in split order.
+// Listed: a token's group of heads over its listed and suffix keys, which needs no merge
+// where it is one split.
 
 #include <math.h>
 
@@ -685,8 +687,7 @@ __global__ __launch_bounds__(256) void batch_merge(BaArgs a, uint16_t* __restric
         merge_row<D, LIST, LPR>(a, sp, (long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR, out, lse);
 }
 
-// float32: rows of one request per workgroup; key c is context key c (or listed key c) below
-// the context count, suffix token c - count from there.
+// float32, listed: key c is listed key c below their count, suffix token c - count from there.
 struct BaF32Args {
     const float *q, *kc, *vc, *ks, *vs;
     int64_t c_sh, c_st, s_ss, s_sh, s_st;
@@ -699,16 +700,11 @@ struct BaF32Args {
     float *part_o, *part_l;          // [split][rows of the step][H] (D)
 };
 
-// Splits of a row tile's keys.
-template <bool LIST>
-__device__ __forceinline__ void f32_split(const BaF32Args& a, const BatchSplit& sp, int& n, int& kps) {
-    n = sp.f32_n;
-    kps = sp.f32_kps;
-    if constexpr (LIST) {
-        batch_split_keys(a.list_tiles + (a.counts[2] + kBaF32Keys - 1) / kBaF32Keys,
-                         sp.rows * a.list_items, kBaF32Wgs, 1, n, kps);
-        kps *= kBaF32Keys;
-    }
+// Listed: splits of an item's keys.
+__device__ __forceinline__ void list_split_f32(const BaF32Args& a, int rows, int& n, int& kps) {
+    batch_split_keys(a.list_tiles + (a.counts[2] + kBaF32Keys - 1) / kBaF32Keys, rows * a.list_items,
+                     kBaF32Wgs, 1, n, kps);
+    kps *= kBaF32Keys;
 }
 
 template <int D, bool LIST>
@@ -719,14 +715,25 @@ __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a
     int* lst = (int*)(f32_lds + sizeof(AttnF32Lds<D, R>));
     const int rl = threadIdx.x % R;
     const BatchSplit sp = load_split(a.counts);
-    int n_split, kps;
-    f32_split<LIST>(a, sp, n_split, kps);
     int x = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+    bool ctx = false;
+    int n_split, kps;
+    if constexpr (LIST) {
+        list_split_f32(a, sp.rows, n_split, kps);
+    } else {
+        const int ctx_wgs = (sp.rows * a.G + R - 1) / R * a.Hkv * sp.f32_n;
+        ctx = x < ctx_wgs;
+        if (!ctx) x -= ctx_wgs;
+        n_split = ctx ? sp.f32_n : sp.f32_sn;
+        kps = ctx ? sp.f32_kps : sp.f32_skps;
+    }
     const int split = x % n_split;
     x /= n_split;
     const int g = x % a.Hkv;
     x /= a.Hkv;
-    int t, hh, seq, own, last_own, n_ctx = a.T;
+    // Keys 0 .. n_ctx - 1 are context keys (or listed ones), the others suffix tokens; the row sees
+    // those up to n_ctx + own, a row of the item those up to n_ctx + last_own.
+    int t, hh, seq, own, last_own, n_ctx = 0;
     bool valid;
     if constexpr (LIST) {
         const int chunks = (a.G + R - 1) / R;
@@ -739,6 +746,15 @@ __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a
         n_ctx = (lst[0] << a.bshift) + lst[1] * a.tail;
         seq = a.row_seq[t];
         own = last_own = a.row_pos[t] - a.T;
+    } else if (ctx) {
+        const int rho0 = x * R + rl, n_th = sp.rows * a.G;
+        valid = rho0 < n_th;
+        const int rho = valid ? rho0 : n_th - 1;
+        t = rho / a.G;
+        hh = rho - t * a.G;
+        seq = 0;
+        n_ctx = a.T;
+        own = last_own = -1;
     } else {
         if (x >= sp.row_tiles) return;
         const BatchTile tl = a.tiles[x];
@@ -755,8 +771,8 @@ __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a
     }
     const uint32_t orow = (uint32_t)t * a.H + g * a.G + hh;
     float *out = a.out, *lse = a.lse;
-    if (n_split > 1) {
-        const size_t part = (size_t)split * sp.rows * a.H;
+    if (!LIST || n_split > 1) {
+        const size_t part = (size_t)(LIST || ctx ? split : sp.f32_n + split) * sp.rows * a.H;
         out = a.part_o + part * D;
         lse = a.part_l + part;
     }
@@ -786,8 +802,8 @@ __global__ __launch_bounds__(256) void batch_merge_f32(BaF32Args a) {
     const int lane = threadIdx.x & 63, grp = lane / LPR, col = lane % LPR;
     const long th = blockIdx.x * 4l + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const BatchSplit sp = load_split(a.counts);
-    int n, kps;
-    f32_split<LIST>(a, sp, n, kps);
+    int n = sp.f32_n + sp.f32_sn, kps;
+    if constexpr (LIST) list_split_f32(a, sp.rows, n, kps);
     const long rows = (long)sp.rows * a.H;
     if (n == 1 || th >= rows) return;
     float M = -INFINITY;
@@ -827,17 +843,28 @@ __global__ __launch_bounds__(256) void batch_merge_f32(BaF32Args a) {
 }  // namespace
 
 // Workgroups of the launch and partial rows of each part: a step of fewer rows than the batch
-// has room for is split further, up to kBaWgs workgroups of kBaRows rows.
-BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_batch& b, int n_sel) {
+// has room for is split further, up to kBaWgs workgroups of kBaRows rows.  float32: never into more
+// splits than its keys fill, since empty workgroups of 16 waves cost too (2 requests over 2732
+// keys: 20.6 us with room for kBaF32Parts workgroups, 14.2).
+BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_batch& b, int block,
+                                     int n_sel) {
     BatchAttnWorkspace w = {};
     if (b.n_rows == 0) return w;
     const long G = p.H / p.H_kv, rows = (long)b.n_rows * p.H;
     if (p.dtype == RELAXKV_DTYPE_F32) {
-        // (with more than one split, kBaF32Wgs workgroups of kBatchRowsF32 rows at most)
-        const long items = (n_sel == 0 ? (long)b.tile_cap
-                                       : b.n_rows * ((G + kBatchRowsF32 - 1) / kBatchRowsF32)) * p.H_kv;
-        const size_t parts = (size_t)kBaF32Wgs * kBatchRowsF32;
-        w.ctx_wgs = (int)(items > kBaF32Wgs ? items : kBaF32Wgs);
+        // (with more than one split, kBaF32Parts workgroups of kBatchRowsF32 rows at most; listed, one
+        // round)
+        const long most = n_sel == 0 ? kBaF32Parts : kBaF32Wgs;
+        auto wgs = [&](long items, long keys) {
+            items *= p.H_kv;
+            const long more = n_sel == 0 ? std::min(items, (long)kBaF32Items) * kBaF32More : 0;
+            return std::min(std::max(items, kBaF32Wgs + more), items * ((keys + kBaF32Keys - 1) / kBaF32Keys));
+        };
+        const size_t parts = n_sel == 0 ? 2 * std::max(most * kBatchRowsF32, rows) : most * kBatchRowsF32;
+        w.ctx_wgs = (int)(n_sel == 0 ? wgs((b.n_rows * G + kBatchRowsF32 - 1) / kBatchRowsF32, p.T_c) +
+                                           wgs(b.tile_cap, b.max_suffix)
+                                     : wgs(b.n_rows * ((G + kBatchRowsF32 - 1) / kBatchRowsF32),
+                                           (long)n_sel * block + b.max_suffix + kBaF32Keys));
         w.part_s_off = parts * p.d * 4;
         w.total = w.part_s_off + parts * 4;
         return w;
@@ -899,7 +926,7 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
         a.scale = scale;
         a.out = (float*)out;
         a.lse = lse_out;
-        const BatchAttnWorkspace w = batch_attn_layout(p, b, n_sel);
+        const BatchAttnWorkspace w = batch_attn_layout(p, b, block, n_sel);
         a.list_items = p.H_kv * ((G + kBatchRowsF32 - 1) / kBatchRowsF32);
         a.list_tiles = (int)(((long)n_sel * block + kBaF32Keys - 1) / kBaF32Keys);
         a.part_o = (float*)ws;
@@ -924,7 +951,7 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
         }
         return hipGetLastError();
     }
-    const BatchAttnWorkspace w = batch_attn_layout(p, b, n_sel);
+    const BatchAttnWorkspace w = batch_attn_layout(p, b, block, n_sel);
     BaArgs a;
     a.q = (const uint16_t*)q;
     a.kc = (const uint16_t*)k_cache + layer_off;

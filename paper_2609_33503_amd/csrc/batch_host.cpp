@@ -109,7 +109,7 @@ relaxkv_status attn(const relaxkv_problem* p, const relaxkv_batch* b, int32_t la
     if (b->n_rows > 0 && (!q || !out || (n_sel && !blocks))) return RELAXKV_EINVAL;
     if (!aligned(k_cache) || !aligned(v_cache) || !aligned(q) || !aligned(out))
         return RELAXKV_EUNSUPPORTED;
-    const BatchAttnWorkspace w = batch_attn_layout(*p, *b, n_sel);
+    const BatchAttnWorkspace w = batch_attn_layout(*p, *b, block, n_sel);
     if (w.total && !ws) return RELAXKV_EINVAL;
     if (ws_bytes < w.total) return RELAXKV_ENOSPACE;
     if ((uintptr_t)ws % 16) return RELAXKV_EUNSUPPORTED;
@@ -207,7 +207,7 @@ relaxkv_status relaxkv_batch_rows(const relaxkv_problem* p, const relaxkv_rope* 
 
 size_t relaxkv_shared_attn_workspace_bytes(const relaxkv_problem* p, const relaxkv_batch* b) {
     if (batch_status(p, b) != RELAXKV_OK) return 0;
-    return batch_attn_layout(*p, *b, 0).total;
+    return batch_attn_layout(*p, *b, 0, 0).total;
 }
 
 relaxkv_status relaxkv_shared_attn(const relaxkv_problem* p, const relaxkv_batch* b, int32_t layer,
@@ -253,7 +253,7 @@ relaxkv_status relaxkv_block_select(const relaxkv_problem* p, const relaxkv_batc
 size_t relaxkv_block_attn_workspace_bytes(const relaxkv_problem* p, const relaxkv_batch* b,
                                           int32_t block, int32_t n_sel) {
     if (batch_status(p, b) != RELAXKV_OK || sel_status(p, block, n_sel) != RELAXKV_OK) return 0;
-    return batch_attn_layout(*p, *b, n_sel).total;
+    return batch_attn_layout(*p, *b, block, n_sel).total;
 }
 
 relaxkv_status relaxkv_block_attn(const relaxkv_problem* p, const relaxkv_batch* b, int32_t layer,
