@@ -73,15 +73,14 @@ template <> struct MfmaF32<16> {
     }
 };
 
-template <int D, int R>
+template <int D, int R, int NW = MfmaF32<R>::waves>
 struct AttnF32Lds {
-    static constexpr int NW = MfmaF32<R>::waves;
     f32x4 q[D * R / 256][64];        // Q fragments: lane l's float4 of d block j
     float o[NW][D][R];               // the waves' outputs, [d][row]
     float m[NW][R], l[NW][R];
 };
 
-// Called by every thread of a workgroup of MfmaF32<R>::waves waves; the lane's row
+// Called by every thread of a workgroup of NW waves; the lane's row
 // is lane % R.  id_of(c) is the source of key c: a row index of kn/vn (row stride
 // fs) when >= 0, else the cached position ~id of kc/vc (row stride cs); all four
 // point at the KV head's first element.  q_row: the lane's query row; lim: its last
@@ -90,15 +89,15 @@ struct AttnF32Lds {
 // n_keys > every row's limit.  The lane's row is row orow of out [][D] and lse_out
 // (may be null); written only if `valid`.  NACC: accumulators of a logit; its products go to
 // them in turn and they are added at the end, so that fewer roundings follow one another.
-template <int D, int R, int NACC = 1, typename IdOf>
-__device__ __forceinline__ void attn_f32_rows(AttnF32Lds<D, R>& sm, const float* kn,
+template <int D, int R, int NACC = 1, int NW = MfmaF32<R>::waves, typename IdOf>
+__device__ __forceinline__ void attn_f32_rows(AttnF32Lds<D, R, NW>& sm, const float* kn,
                                               const float* vn, int64_t fs, const float* kc,
                                               const float* vc, int64_t cs, IdOf id_of, int n_keys,
                                               const float* q_row, int lim, float scale, bool valid,
                                               float* out, float* lse_out, uint32_t orow) {
     typedef MfmaF32<R> M32;
     typedef typename M32::Acc Acc;
-    constexpr int NW = M32::waves, NG = 64 / R, NV = sizeof(Acc) / 4;
+    constexpr int NG = 64 / R, NV = sizeof(Acc) / 4;
     constexpr int J = D / (4 * NG), DB = D / R;
     const int tid = threadIdx.x, lane = tid & 63, rl = lane % R, grp = lane / R;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);

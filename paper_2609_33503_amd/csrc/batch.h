@@ -37,10 +37,15 @@ constexpr int kBaItemWgs = 512;        // of them for context items that one wor
 constexpr int kBaMinTiles = 8;         // fewest tiles per split
 constexpr int kBaXcds = 8;
 constexpr int kBaLongSuffix = 1024;    // tokens from which the suffix items go first
-// float32: a split's keys are at least one block for each of the 16 waves; one workgroup per CU
-// (at d 128); up to kBaF32More splits more where as many as kBaF32Items items leave CUs of the
-// last round idle (64 requests of 5 rows, 8 heads, over 8K: 157 us, 197 without; over 32K 543, 778).
-constexpr int kBaF32Keys = 256, kBaF32Wgs = 256, kBaF32Items = 512, kBaF32More = 3;
+// float32: workgroups of 8 waves, listed 4, so that two or four share a CU and one's start and end
+// pass beside another's keys (33 requests of 4 rows, 3 heads, over 2097 keys: 15.4 us, 21.4 with 16
+// waves, 14.8 and a longer merge with 4; 65 rows of 8 heads over 200 listed and suffix keys: 18.3,
+// 20.5 with 8, 29.0 with 16).  A split's keys are at least one 16-key block for each wave.  Shared:
+// up to kBaF32More splits more where as many as kBaF32Items items leave places of the last round
+// idle (64 requests of 5 rows, 8 heads, over 32K: 543 us, 778 without).
+constexpr int kBaF32Waves = 8, kBaF32ListWaves = 4;
+constexpr int kBaF32Keys = 16 * kBaF32Waves, kBaF32ListKeys = 16 * kBaF32ListWaves;
+constexpr int kBaF32Wgs = 256, kBaF32ListWgs = 512, kBaF32Items = 512, kBaF32More = 3;
 constexpr int kBaF32Parts = kBaF32Wgs + kBaF32More * kBaF32Items;     // workgroups of several splits
 constexpr int kBatchSplitAt = 16;      // first word of the split in relaxkv_batch::counts
 

@@ -694,7 +694,7 @@ struct BaF32Args {
     const int32_t *counts, *row_seq, *row_pos, *lists;
     const BatchTile* tiles;
     int T, H, Hkv, G, n_sel, bshift, nb, tail;
-    int list_tiles, list_items;      // listed: kBaF32Keys of a row at most (and its suffix), items
+    int list_tiles, list_items;      // listed: kBaF32ListKeys of a row at most, items of a token
     float scale;
     float *out, *lse;
     float *part_o, *part_l;          // [split][rows of the step][H] (D)
@@ -702,17 +702,19 @@ struct BaF32Args {
 
 // Listed: splits of an item's keys.
 __device__ __forceinline__ void list_split_f32(const BaF32Args& a, int rows, int& n, int& kps) {
-    batch_split_keys(a.list_tiles + (a.counts[2] + kBaF32Keys - 1) / kBaF32Keys, rows * a.list_items,
-                     kBaF32Wgs, 1, n, kps);
-    kps *= kBaF32Keys;
+    batch_split_keys(a.list_tiles + (a.counts[2] + kBaF32ListKeys - 1) / kBaF32ListKeys,
+                     rows * a.list_items, kBaF32ListWgs, 1, n, kps);
+    kps *= kBaF32ListKeys;
 }
 
+template <bool LIST> constexpr int f32_waves() { return LIST ? kBaF32ListWaves : kBaF32Waves; }
 template <int D, bool LIST>
-__global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a) {
-    constexpr int R = kBatchRowsF32;
+__global__ __launch_bounds__(f32_waves<LIST>() * 64, 4) void battn_f32(BaF32Args a) {
+    constexpr int R = kBatchRowsF32, NW = f32_waves<LIST>();
     extern __shared__ __attribute__((aligned(16))) char f32_lds[];
-    AttnF32Lds<D, R>& sm = *(AttnF32Lds<D, R>*)f32_lds;
-    int* lst = (int*)(f32_lds + sizeof(AttnF32Lds<D, R>));
+    typedef AttnF32Lds<D, R, NW> Lds;
+    Lds& sm = *(Lds*)f32_lds;
+    int* lst = (int*)(f32_lds + sizeof(Lds));
     const int rl = threadIdx.x % R;
     const BatchSplit sp = load_split(a.counts);
     int x = (int)(blockIdx.y * gridDim.x + blockIdx.x);
@@ -789,9 +791,9 @@ __global__ __launch_bounds__(MfmaF32<16>::waves * 64) void battn_f32(BaF32Args a
         else return ~c;
     };
     const int64_t sb = seq * a.s_ss + g * a.s_sh;
-    attn_f32_rows<D, R, 4>(sm, a.ks + sb, a.vs + sb, a.s_st, a.kc + g * a.c_sh, a.vc + g * a.c_sh,
-                           a.c_st, id_of, n_keys, a.q + (size_t)orow * D,
-                           max(-1, min(n_keys - 1, n_ctx + own - key0)), a.scale, valid, out, lse, orow);
+    attn_f32_rows<D, R, 4, NW>(sm, a.ks + sb, a.vs + sb, a.s_st, a.kc + g * a.c_sh, a.vc + g * a.c_sh,
+                               a.c_st, id_of, n_keys, a.q + (size_t)orow * D,
+                               max(-1, min(n_keys - 1, n_ctx + own - key0)), a.scale, valid, out, lse, orow);
 }
 
 // One wave per (token, head): lane s takes split s's log-sum-exp, D/4 lanes (twice at d 64) then
@@ -819,7 +821,7 @@ __global__ __launch_bounds__(256) void batch_merge_f32(BaF32Args a) {
         const float w = c0 + lane < n ? expf(a.part_l[(c0 + lane) * rows + th] - ref) : 0.f;
         z += w;
         const int m = min(64, n - c0);
-#pragma unroll 4
+#pragma unroll 8
         for (int j0 = 0; j0 < m; j0 += NG) {
             const int j = min(j0 + grp, m - 1);
             float wj = __shfl(w, j, 64);
@@ -844,8 +846,8 @@ __global__ __launch_bounds__(256) void batch_merge_f32(BaF32Args a) {
 
 // Workgroups of the launch and partial rows of each part: a step of fewer rows than the batch
 // has room for is split further, up to kBaWgs workgroups of kBaRows rows.  float32: never into more
-// splits than its keys fill, since empty workgroups of 16 waves cost too (2 requests over 2732
-// keys: 20.6 us with room for kBaF32Parts workgroups, 14.2).
+// splits than its keys fill, since empty workgroups cost too (of 16 waves, 2 requests over 2732
+// keys: 20.6 us with room for kBaF32Parts of them, 14.2).
 BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_batch& b, int block,
                                      int n_sel) {
     BatchAttnWorkspace w = {};
@@ -854,17 +856,18 @@ BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_bat
     if (p.dtype == RELAXKV_DTYPE_F32) {
         // (with more than one split, kBaF32Parts workgroups of kBatchRowsF32 rows at most; listed, one
         // round)
-        const long most = n_sel == 0 ? kBaF32Parts : kBaF32Wgs;
+        const long most = n_sel == 0 ? kBaF32Parts : kBaF32ListWgs;
         auto wgs = [&](long items, long keys) {
+            const int unit = n_sel == 0 ? kBaF32Keys : kBaF32ListKeys;
             items *= p.H_kv;
-            const long more = n_sel == 0 ? std::min(items, (long)kBaF32Items) * kBaF32More : 0;
-            return std::min(std::max(items, kBaF32Wgs + more), items * ((keys + kBaF32Keys - 1) / kBaF32Keys));
+            const long round = n_sel == 0 ? kBaF32Wgs + std::min(items, (long)kBaF32Items) * kBaF32More : most;
+            return std::min(std::max(items, round), items * ((keys + unit - 1) / unit));
         };
         const size_t parts = n_sel == 0 ? 2 * std::max(most * kBatchRowsF32, rows) : most * kBatchRowsF32;
         w.ctx_wgs = (int)(n_sel == 0 ? wgs((b.n_rows * G + kBatchRowsF32 - 1) / kBatchRowsF32, p.T_c) +
                                            wgs(b.tile_cap, b.max_suffix)
                                      : wgs(b.n_rows * ((G + kBatchRowsF32 - 1) / kBatchRowsF32),
-                                           (long)n_sel * block + b.max_suffix + kBaF32Keys));
+                                           (long)n_sel * block + b.max_suffix + kBaF32ListKeys));
         w.part_s_off = parts * p.d * 4;
         w.total = w.part_s_off + parts * 4;
         return w;
@@ -928,7 +931,7 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
         a.lse = lse_out;
         const BatchAttnWorkspace w = batch_attn_layout(p, b, block, n_sel);
         a.list_items = p.H_kv * ((G + kBatchRowsF32 - 1) / kBatchRowsF32);
-        a.list_tiles = (int)(((long)n_sel * block + kBaF32Keys - 1) / kBaF32Keys);
+        a.list_tiles = (int)(((long)n_sel * block + kBaF32ListKeys - 1) / kBaF32ListKeys);
         a.part_o = (float*)ws;
         a.part_l = (float*)(ws + w.part_s_off);
         auto go = [&](auto d_t, auto list_t) {
@@ -936,8 +939,8 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
             constexpr bool LIST = decltype(list_t)::value;
             // (a launch dimension holds fewer than 2^32 threads)
             const unsigned nx = std::min(w.ctx_wgs, 1 << 20);
-            hipLaunchKernelGGL((battn_f32<D, LIST>), dim3(nx, (w.ctx_wgs + nx - 1) / nx), dim3(MfmaF32<16>::waves * 64),
-                               sizeof(AttnF32Lds<D, kBatchRowsF32>) + (LIST ? (n_sel + 2) * sizeof(int) : 0),
+            hipLaunchKernelGGL((battn_f32<D, LIST>), dim3(nx, (w.ctx_wgs + nx - 1) / nx), dim3(f32_waves<LIST>() * 64),
+                               sizeof(AttnF32Lds<D, kBatchRowsF32, f32_waves<LIST>()>) + (LIST ? (n_sel + 2) * sizeof(int) : 0),
                                st, a);
             hipLaunchKernelGGL((batch_merge_f32<D, LIST>), dim3((unsigned)(((long)b.n_rows * p.H + 3) / 4)),
                                dim3(256), 0, st, a);

@@ -176,6 +176,21 @@ def test_lowest_keys(gpu_lib, low):
     s.check(ref)
 
 
+@pytest.mark.parametrize("low", [float("-inf"), torch.finfo(F32).min, -1e30])
+def test_lowest_keys_f32(gpu_lib, low):
+    """The same in float32, in more splits than have another key, and among listed blocks."""
+    s = Step(past=[30, 2], new=[1, 2], T=1000, seed=6, dtype=F32)
+    s.q[..., 0] = 1.0
+    s.kc[:, :, 64:900, 0] = low
+    s.kc[:, :, 0, 0] = low
+    ref = s.reference()
+    s.shared()
+    s.check(ref)
+    lists = torch.arange(16, dtype=torch.int32, device="cuda").expand(3, 2, 16).contiguous()
+    s.blocks(64, lists)
+    s.check(s.reference(lists, 64))
+
+
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("T,block", [(640, None), (640, 64), (20, None), (9000, None)])
 def test_not_finite_reaches_the_rows_that_see_it(gpu_lib, T, block, dtype):

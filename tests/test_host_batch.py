@@ -231,15 +231,15 @@ def test_workspace_sizes(rk):
     assert lib.relaxkv_block_select_workspace_bytes(ctypes.byref(p), ctypes.byref(b), 40) == 0
     assert lib.relaxkv_block_attn_workspace_bytes(ctypes.byref(p), ctypes.byref(b), 64, 513) == 0
     assert lib.relaxkv_block_attn_workspace_bytes(ctypes.byref(p), ctypes.byref(b), 64, 512) > 0
-    # float32: 256 workgroups of 16 rows, d values and a log-sum-exp each; shared context: three
-    # times 512 more, or the rows if more, and twice
+    # float32: workgroups of 16 rows, d values and a log-sum-exp each: listed 512; shared context
+    # 256 and three times 512, or the rows if more, and twice
     p = _problem(rk, dtype=0)
     for n_rows in (1, 3000):
         b = _batch(rk, p, n_rows=n_rows)
         assert lib.relaxkv_shared_attn_workspace_bytes(ctypes.byref(p), ctypes.byref(b)) == \
             2 * max((256 + 3 * 512) * 16, n_rows * 8) * (128 * 4 + 4)
         assert lib.relaxkv_block_attn_workspace_bytes(ctypes.byref(p), ctypes.byref(b), 64, 3) == \
-            256 * 16 * (128 * 4 + 4)
+            512 * 16 * (128 * 4 + 4)
     b = _batch(rk, p, n_rows=0)
     assert lib.relaxkv_shared_attn_workspace_bytes(ctypes.byref(p), ctypes.byref(b)) == 0
 
