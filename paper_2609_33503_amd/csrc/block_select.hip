@@ -13,7 +13,7 @@
 // per row and KV head, against 4 G d per key of the attention that follows.
 //
 // block_means is memory bound (reads every key once: 40 layers of 8 heads, 16K keys, d 128 in 234 us,
-// 5.8 TB/s); the scores' products are few (8 rows and 8 heads, 2048 blocks, d 128: 6.1 us, of
+// 5.8 TB/s); the scores' products are few (8 rows and 8 heads, 2048 blocks, d 128: 4.3 us, of
 // which the launch and the first loads are most), and the top-k of up to 4096 blocks keeps its
 // keys in registers.
 
@@ -94,27 +94,33 @@ __global__ __launch_bounds__(256) void block_means(const T* __restrict__ k, KvSt
     }
 }
 
-constexpr int kScoreTokens = 8;        // rows a workgroup scores against its 64 blocks
-
-// Four lanes per block, each a quarter of the head dimension in 8-element chunks.
+// 16 rows against 64 blocks of a KV head per workgroup, on the 64-bit matrix instruction (16x16x4):
+// a wave takes 16 blocks, lane r + 16 k the elements [k d/4, (k + 1) d/4) of row r's summed queries
+// and of block r's mean, so that step i multiplies element k d/4 + i for the four k.
+// (58 rows and 8 heads, 3125 blocks, d 128: 16.8 us; with vector multiply-adds, whose queries
+// come from LDS two at a time, 24.)
+constexpr int kScoreRows = 16;
 template <typename T, int D>
 __global__ __launch_bounds__(256) void block_scores(const T* __restrict__ q,
                                                     const T* __restrict__ means,
                                                     const int32_t* __restrict__ counts, int n_rows,
                                                     int H, int Hkv, int G, int nb,
                                                     float* __restrict__ scores) {
-    constexpr int NT = kScoreTokens;
-    __shared__ __attribute__((aligned(16))) double qs[NT][D];
-    const int tid = threadIdx.x, g = blockIdx.y, t0 = blockIdx.z * NT;
-    const int part = tid & 3, b = blockIdx.x * 64 + (tid >> 2);
-    const T* m = means + ((size_t)g * nb + min(b, nb - 1)) * D;
-    float mf[8];
-    load8<T>(m + part * 8, mf);
+    typedef double f64x4 __attribute__((ext_vector_type(4)));
+    typedef double f64x2 __attribute__((ext_vector_type(2)));
+    constexpr int NR = kScoreRows, KD = D / 4;
+    __shared__ __attribute__((aligned(16))) double qs[NR][D + 2];     // (rows in different banks)
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, kk = lane >> 4;
+    const int g = blockIdx.y, t0 = blockIdx.z * NR, b = (blockIdx.x * 4 + (tid >> 6)) * 16 + r;
+    const T* m = means + ((size_t)g * nb + min(b, nb - 1)) * D + kk * KD;
+    float mf[KD];
+#pragma unroll
+    for (int i = 0; i < KD; i += 8) load8<T>(m + i, mf + i);
     const int rows = min(counts[0], n_rows);
     if (t0 >= rows) return;
     // The summed group queries: 8 elements of one row per thread, the heads' loads in flight
     // together.
-    for (int x = tid; x < NT * D / 8; x += 256) {
+    for (int x = tid; x < NR * D / 8; x += 256) {
         const int t = x / (D / 8), c = (x - t * (D / 8)) * 8;
         double s[8];
 #pragma unroll
@@ -135,29 +141,18 @@ __global__ __launch_bounds__(256) void block_scores(const T* __restrict__ q,
         for (int e = 0; e < 8; ++e) qs[t][c + e] = s[e];
     }
     __syncthreads();
-    double acc[NT];
+    f64x4 acc = {0.0, 0.0, 0.0, 0.0}, acc1 = acc;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = 0.0;
-#pragma unroll 1
-    for (int i = 0; i < D / 32; ++i) {                     // (not unrolled, for the registers)
-        const int c0 = (part + 4 * i) * 8;
-        float nf[8];
-        if (i + 1 < D / 32) load8<T>(m + c0 + 32, nf);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const double x = (double)mf[e];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) acc[t] = fma(qs[t][c0 + e], x, acc[t]);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) mf[e] = nf[e];
+    for (int i = 0; i < KD; i += 2) {
+        const f64x2 a = *(const f64x2*)&qs[r][kk * KD + i];
+        acc = __builtin_amdgcn_mfma_f64_16x16x4f64(a[0], (double)mf[i], acc, 0, 0, 0);
+        acc1 = __builtin_amdgcn_mfma_f64_16x16x4f64(a[1], (double)mf[i + 1], acc1, 0, 0, 0);
     }
+    acc += acc1;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        acc[t] += __shfl_xor(acc[t], 1, 64);
-        acc[t] += __shfl_xor(acc[t], 2, 64);
-        if (part == (t & 3) && b < nb && t0 + t < rows)
-            scores[((size_t)(t0 + t) * Hkv + g) * nb + b] = (float)acc[t];
+    for (int v = 0; v < 4; ++v) {                        // (row kk + 4 v, block r)
+        const int t = t0 + kk + 4 * v;
+        if (b < nb && t < rows) scores[((size_t)t * Hkv + g) * nb + b] = (float)acc[v];
     }
 }
 
@@ -180,15 +175,16 @@ __device__ __forceinline__ int wave_scan_dpp(int x) {
     return x;
 }
 
-// The k largest of a row's keys, by a workgroup of W waves: wave w holds the 8 * 64 blocks from
-// w * 512, block e * 64 + lane of them in register e.  The k-th largest key is found 8 bits at
+// The k largest of a row's keys, by a workgroup of W waves: wave w holds the E * 64 blocks from
+// w * E * 64, block e * 64 + lane of them in register e.  The k-th largest key is found 8 bits at
 // a time from a histogram in LDS of the keys that share the bits found so far, in four copies
 // (scores share few exponents, and an atomic takes a turn per lane of the same address); the
 // next digit's histogram is cleared while this one is summed.  Blocks past the row's end hold
 // key 0; a NaN's key 0 lies at a lower block, and k is at most the row's length, so none of
 // them is ever taken.
-// (2048 blocks, 64 rows of KV heads, k 32: 5.6 us; two bits at a time by counting keys in every
-// wave 11.4, one wave per row and one bit at a time by ballots 42.)
+// (2048 blocks, 64 rows of KV heads, k 32: 5.2 us with 8 waves, 5.8 with 4; 500 blocks 4.7 with 4
+// waves, 6.5 with one; two bits at a time by counting keys in every wave 11.4, one wave per row and
+// one bit at a time by ballots 42.)
 template <int W>
 struct TopkLds {
     int hist[2][4][256];
@@ -196,9 +192,9 @@ struct TopkLds {
     uint32_t part[W];
 };
 
-template <int W, int NT = W * 64>          // (NT: threads of the workgroup)
-__device__ __forceinline__ void topk_keys(TopkLds<W>& sm, const uint32_t (&key)[8], int k, int32_t* out) {
-    constexpr int E = 8, COPIES = 4;
+template <int W, int E, int NT = W * 64>   // (NT: threads of the workgroup)
+__device__ __forceinline__ void topk_keys(TopkLds<W>& sm, const uint32_t (&key)[E], int k, int32_t* out) {
+    constexpr int COPIES = 4;
     constexpr int SW = W < 4 ? W : 4, BPT = 256 / (SW * 64);   // waves that sum, bins per thread
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -280,39 +276,44 @@ __device__ __forceinline__ void topk_keys(TopkLds<W>& sm, const uint32_t (&key)[
 }
 
 // One workgroup per (row, KV head) over scores in memory.
-template <int W>
+template <int W, int E>
 __global__ __launch_bounds__(W * 64) void block_topk_reg(const float* __restrict__ scores, int nb,
                                                          int k, const int32_t* __restrict__ counts,
                                                          int n_rows, int Hkv,
                                                          int32_t* __restrict__ out) {
     __shared__ TopkLds<W> sm;
     const long unit = blockIdx.x;
-    const int i0 = (threadIdx.x >> 6) * 512 + (threadIdx.x & 63);
+    const int i0 = (threadIdx.x >> 6) * (E * 64) + (threadIdx.x & 63);
     const float* s = scores + unit * nb;                 // (within the workspace for every unit)
-    float x[8];
+    float x[E];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = i0 + e * 64 < nb ? s[i0 + e * 64] : 0.f;
+    for (int e = 0; e < E; ++e) x[e] = i0 + e * 64 < nb ? s[i0 + e * 64] : 0.f;
     if (unit >= (long)min(counts[0], n_rows) * Hkv) return;
-    uint32_t key[8];
+    uint32_t key[E];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) key[e] = i0 + e * 64 < nb ? score_key(x[e]) : 0u;
-    topk_keys<W>(sm, key, k, out + unit * k);
+    for (int e = 0; e < E; ++e) key[e] = i0 + e * 64 < nb ? score_key(x[e]) : 0u;
+    topk_keys<W, E>(sm, key, k, out + unit * k);
 }
 
 // Scores and top-k of one (row, KV head) in one workgroup: for steps of few rows, which are
-// bound by the latency of a launch and not by a CU's 64-bit products (97 rows of 2 KV heads, 512
-// blocks, d 64: 7.1 us for 5.2 + 6.0 in two launches; but 8 rows of 8 heads, 2048 blocks, d 128:
-// 24.2 us for 6.2 + 5.6).  Four lanes per block, each a quarter of the head dimension.
+// bound by the latency of a launch and not by a CU's 64-bit products (84 rows of KV heads, 511
+// blocks, d 64: 7.3 us for 4.7 + 5.0 in two launches; 240, 1000 blocks: 7.5 for 4.4 + 5.5; 240, 500
+// blocks, d 128: 9.9 for 4.4 + 5.4; 64, 2048 blocks, d 128: 24 for 4.3 + 5.2).  Four lanes per block, each a quarter of the head dimension.
 constexpr int kFusedThreads = 1024;
-template <typename T, int D, int W>
+// Steps that take one launch: products per row (blocks times d), and units (rows times KV
+// heads) of one round of workgroups.
+constexpr long kFusedProducts = 65536, kFusedUnits = 256;
+template <typename T, int D>
 __global__ __launch_bounds__(kFusedThreads) void block_select_rows(const T* __restrict__ q,
                                                             const T* __restrict__ means, int nb, int k,
                                                             const int32_t* __restrict__ counts,
                                                             int n_rows, int H, int Hkv, int G,
                                                             int32_t* __restrict__ out) {
     constexpr int NT = kFusedThreads, NC = D / 32, BLK = NT / 4;   // chunks of a lane, blocks at a time
+    constexpr int W = NT / 64;                           // (one block per thread in the top-k)
+    static_assert(kFusedProducts <= NT * 64, "a row's blocks have a thread each");
     __shared__ TopkLds<W> sm;
-    __shared__ float score[512 * W];
+    __shared__ float score[NT];
     __shared__ __attribute__((aligned(16))) double qs[D];
     const int tid = threadIdx.x, part = tid & 3;
     const int t = blockIdx.x / Hkv, g = blockIdx.x - t * Hkv;
@@ -354,16 +355,9 @@ __global__ __launch_bounds__(kFusedThreads) void block_select_rows(const T* __re
         if (part == 0 && b < nb) score[b] = (float)s;
     }
     __syncthreads();
-    const int i0 = (tid >> 6) * 512 + (tid & 63);
-    uint32_t key[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) key[e] = i0 + e * 64 < nb ? score_key(score[min(i0 + e * 64, nb - 1)]) : 0u;
-    topk_keys<W, NT>(sm, key, k, out + (size_t)blockIdx.x * k);
+    const uint32_t key[1] = {tid < nb ? score_key(score[min(tid, nb - 1)]) : 0u};
+    topk_keys<W, 1>(sm, key, k, out + (size_t)blockIdx.x * k);
 }
-
-// Steps that take one launch: products per row (blocks times d), and units (rows times KV
-// heads) of one round of workgroups.
-constexpr long kFusedProducts = 65536, kFusedUnits = 256;
 
 // Rows of any length: one workgroup per (row, KV head) reads its scores once per 8-bit
 // digit and once for the compaction.
@@ -429,7 +423,7 @@ void launch_scores(const relaxkv_problem& p, const relaxkv_batch& b, int block, 
                    const void* q, float* scores, hipStream_t st) {
     const int nb = block_count(p, block);
     hipLaunchKernelGGL((block_scores<T, D>),
-                       dim3((nb + 63) / 64, p.H_kv, (b.n_rows + kScoreTokens - 1) / kScoreTokens),
+                       dim3((nb + 63) / 64, p.H_kv, (b.n_rows + kScoreRows - 1) / kScoreRows),
                        dim3(256), 0, st, (const T*)q, (const T*)means, b.counts, b.n_rows, p.H,
                        p.H_kv, p.H / p.H_kv, nb, scores);
 }
@@ -466,9 +460,8 @@ hipError_t launch_block_select(const relaxkv_problem& p, const relaxkv_batch& b,
         };
         auto go_t = [&](auto q_t) {
             typedef decltype(q_t) T;
-            if (p.d == 128) go(block_select_rows<T, 128, 1>, q_t);
-            else if (nb <= 512) go(block_select_rows<T, 64, 1>, q_t);
-            else go(block_select_rows<T, 64, 2>, q_t);
+            if (p.d == 128) go(block_select_rows<T, 128>, q_t);
+            else go(block_select_rows<T, 64>, q_t);
         };
         if (p.dtype == RELAXKV_DTYPE_BF16) go_t(uint16_t{});
         else go_t(float{});
@@ -485,10 +478,10 @@ hipError_t launch_block_select(const relaxkv_problem& p, const relaxkv_batch& b,
         hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3(waves * 64), 0, st, scores, nb, n_sel,
                            b.counts, b.n_rows, p.H_kv, blocks);
     };
-    if (nb <= 512) go(block_topk_reg<1>, 1);
-    else if (nb <= 1024) go(block_topk_reg<2>, 2);
-    else if (nb <= 2048) go(block_topk_reg<4>, 4);
-    else if (nb <= 4096) go(block_topk_reg<8>, 8);
+    if (nb <= 512) go(block_topk_reg<4, 2>, 4);
+    else if (nb <= 1024) go(block_topk_reg<8, 2>, 8);
+    else if (nb <= 2048) go(block_topk_reg<8, 4>, 8);
+    else if (nb <= 4096) go(block_topk_reg<16, 4>, 16);
     else go(block_topk_long, 4);
     return hipGetLastError();
 }
