@@ -540,6 +540,8 @@ class Request:
                              f"cuda:{_current_device()}")
         if stream is not None and stream.device_index != self._index:
             raise ValueError(f"the stream is not on {self.device}")
+        if stream is None and _raw_stream is not None:    # (the request's tensors are on the GPU)
+            return _raw_stream(self._index)
         return _stream(stream)
 
     def _batch(self, batch):

@@ -454,6 +454,29 @@ def test_offsets_past_32_bits(gpu_lib, dtype):
     assert torch.equal(mean[-1, :, -m:], one[0]) and not mean[:-1].any() and not mean[-1, :, :-m].any()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_steps_without_rows(gpu_lib, dtype):
+    """A batch with no room for rows, and a step in which every request rests: nothing is
+    written."""
+    for new, extra in (([0, 0], 0), ([0, 0], 5)):
+        s = Step(past=[7, 0], new=new, T=100, dtype=dtype, extra_rows=extra, room=9)
+        assert s.batch.counts_to_host() == [0, 0, 0, 0]
+        assert s.batch.row_off.tolist() == [0, 0, 0] and s.batch.row_seq.tolist() == [-1] * extra
+        n = s.q.shape[0]
+        k = torch.zeros(n, 2, 128, dtype=dtype, device="cuda")
+        ks, vs, q_rot = s.ks.clone(), s.vs.clone(), torch.full_like(s.q, 7.0)
+        s.req.batch_rows(relaxkv.Rope(), s.batch, s.q, k, k, q_rot, s.ks, s.vs)
+        s.shared()
+        lists = torch.full((n, 2, 3), -7, dtype=torch.int32, device="cuda")
+        means = torch.zeros(2, 7, 128, dtype=dtype, device="cuda")
+        ws = s.req.alloc_block_workspace(s.batch, 16, 3)
+        s.req.block_select(s.batch, 16, means, s.q, lists, ws)
+        s.blocks(16, lists)
+        assert torch.equal(ks.nan_to_num(9), s.ks.nan_to_num(9)) and torch.equal(vs.nan_to_num(9), s.vs.nan_to_num(9))
+        for t, v in ((q_rot, 7), (s.out, 7), (s.lse, 7), (lists, -7)):
+            assert bool((t == v).all())
+
+
 def test_expanded_suffix_is_refused(gpu_lib):
     """A stride of 0 (an expanded tensor) selects the dense layout in the descriptor, so it must
     not get there."""
