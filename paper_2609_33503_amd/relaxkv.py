@@ -226,8 +226,9 @@ def _stream(stream):
 
 
 def _dense(t, dtype, shape, index):
-    """A plain contiguous tensor of this dtype and shape on GPU `index`."""
-    return (type(t) is _Tensor and t.dtype is dtype and t.shape == shape and t.is_cuda
+    """A plain contiguous tensor of this dtype and shape on GPU `index` (get_device() is -1 for
+    a host tensor)."""
+    return (type(t) is _Tensor and t.dtype is dtype and t.shape == shape
             and t.get_device() == index and t.is_contiguous())
 
 
@@ -362,7 +363,7 @@ class Request:
 
     def _caches(self, k_cache, v_cache):
         for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-            if not (type(t) is _Tensor and t.dtype is self.dtype and t.is_cuda
+            if not (type(t) is _Tensor and t.dtype is self.dtype
                     and t.get_device() == self._index and t.shape == self._cache_shape
                     and t.stride() == self._cache_stride):
                 _need_cache(t, name, self.dtype, self._cache_shape, self.device, self.kv_strides)
@@ -373,8 +374,7 @@ class Request:
             raise ValueError("sets must come from alloc_sets() of a request of this shape")
 
     def _ws(self, ws, name="ws"):
-        if type(ws) is _Tensor and ws.is_cuda and ws.get_device() == self._index and \
-                ws.is_contiguous():
+        if type(ws) is _Tensor and ws.get_device() == self._index and ws.is_contiguous():
             return
         if not isinstance(ws, torch.Tensor) or ws.device != self.device or not ws.is_contiguous():
             raise ValueError(f"{name} must be a contiguous tensor on {self.device}")
@@ -552,12 +552,14 @@ class Request:
         """The suffix caches' descriptor (the library checks the strides)."""
         shape = batch.suffix_shape
         for t, name in ((k, "k_suffix"), (v, "v_suffix")):
-            if not (type(t) is _Tensor and t.dtype is self.dtype and t.shape == shape and t.is_cuda
-                    and t.get_device() == self._index and t.stride(3) == 1):
+            if not (type(t) is _Tensor and t.dtype is self.dtype and t.shape == shape
+                    and t.get_device() == self._index):
                 _need_cache(t, name, self.dtype, shape, self.device)
         st = k.stride()
-        if st != v.stride() or batch.flat or 0 in st:     # (a dimension of size 1: any stride)
-            st = _cache_strides(k)
+        if st != v.stride() or batch.flat or 0 in st or st[3] != 1:
+            for t, name in ((k, "k_suffix"), (v, "v_suffix")):
+                _need_cache(t, name, self.dtype, shape, self.device)
+            st = _cache_strides(k)                        # (a dimension of size 1: any stride)
             if st != _cache_strides(v):
                 raise ValueError("k_suffix and v_suffix must have the same strides")
         return CSuffix(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2])
@@ -566,8 +568,8 @@ class Request:
         """The row stride of a [n][heads][d] tensor whose rows are contiguous."""
         if t is None:
             return 0
-        if type(t) is _Tensor and t.dtype is self.dtype and t.is_cuda \
-                and t.get_device() == self._index and t.shape == (n, heads, self.d):
+        if type(t) is _Tensor and t.dtype is self.dtype and t.get_device() == self._index \
+                and t.shape == (n, heads, self.d):
             st = t.stride()
             if st[2] == 1 and st[1] == self.d and n > 1 and st[0] > 0:
                 return st[0]
@@ -651,11 +653,12 @@ class Request:
     def _batch_attn(self, batch, k_cache, v_cache, q, out, lse_out, ws):
         self._batch(batch)
         self._caches(k_cache, v_cache)
-        shape = (batch.n_rows, self.H, self.d)
-        self._want(q, "q", self.dtype, shape)
-        self._want(out, "out", self.dtype, shape)
-        if lse_out is not None:
-            self._want(lse_out, "lse_out", torch.float32, shape[:2])
+        shape, dtype, index = batch.q_shape, self.dtype, self._index
+        if not (_dense(q, dtype, shape, index) and _dense(out, dtype, shape, index)):
+            self._want(q, "q", dtype, shape)
+            self._want(out, "out", dtype, shape)
+        if lse_out is not None and not _dense(lse_out, torch.float32, batch.lse_shape, index):
+            self._want(lse_out, "lse_out", torch.float32, batch.lse_shape)
         if ws is not None:
             self._ws(ws)
 
@@ -774,6 +777,7 @@ class Batch:
         self.key = (req.T_c, req.H, req.H_kv, req.d, req.dtype, req._index)
         self.suffix_shape = (s.n_seq, req.H_kv, s.max_suffix, req.d)
         self.flat = 1 in self.suffix_shape[:3]
+        self.q_shape, self.lse_shape = (s.n_rows, req.H, req.d), (s.n_rows, req.H)
         base = buf.data_ptr()
 
         def view(ptr, n):
