@@ -46,7 +46,14 @@ constexpr int kBaLongSuffix = 1024;    // tokens from which the suffix items go 
 constexpr int kBaF32Waves = 8, kBaF32ListWaves = 4;
 constexpr int kBaF32Keys = 16 * kBaF32Waves, kBaF32ListKeys = 16 * kBaF32ListWaves;
 constexpr int kBaF32Wgs = 256, kBaF32ListWgs = 512, kBaF32Items = 512, kBaF32More = 3;
-constexpr int kBaF32Parts = kBaF32Wgs + kBaF32More * kBaF32Items;     // workgroups of several splits
+// Workgroups of several splits: below kBaF32Wgs items at most kBaF32Wgs and kBaF32More per item.  Above,
+// n splits of an item are taken only where their rounds r of kBaF32Wgs workgroups are fewer than
+// 2 n, those of one split each (r (units / n + 1) < 2 (units + 1)), so they are at most 2 n - 1 rounds:
+// seven with four splits.
+constexpr int kBaF32Parts = kBaF32Wgs + kBaF32More * kBaF32Items;
+static_assert(kBaF32Items == 2 * kBaF32Wgs && kBaF32Parts >= (2 * (kBaF32More + 1) - 1) * kBaF32Wgs &&
+                  kBaF32Parts >= (1 + kBaF32More) * kBaF32Wgs,
+              "the splits of every step fit");
 constexpr int kBatchSplitAt = 16;      // first word of the split in relaxkv_batch::counts
 
 // Shared context: item (g, chunk) = g * chunks + chunk holds `tiles` key tiles, worker w takes

@@ -860,7 +860,10 @@ BatchAttnWorkspace batch_attn_layout(const relaxkv_problem& p, const relaxkv_bat
         auto wgs = [&](long items, long keys) {
             const int unit = n_sel == 0 ? kBaF32Keys : kBaF32ListKeys;
             items *= p.H_kv;
-            const long round = n_sel == 0 ? kBaF32Wgs + std::min(items, (long)kBaF32Items) * kBaF32More : most;
+            // (a step of i <= items takes one split, or as many as are kBaF32Wgs workgroups, and
+            // kBaF32More)
+            const long i = std::min(items, (long)kBaF32Items);
+            const long round = n_sel == 0 ? std::min(std::max(i, (long)kBaF32Wgs) + i * kBaF32More, most) : most;
             return std::min(std::max(items, round), items * ((keys + unit - 1) / unit));
         };
         const size_t parts = n_sel == 0 ? 2 * std::max(most * kBatchRowsF32, rows) : most * kBatchRowsF32;
