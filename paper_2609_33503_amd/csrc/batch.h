@@ -146,7 +146,7 @@ __host__ __device__ inline BatchSplit batch_split(int rows, int row_tiles, int l
     return s;
 }
 
-// Scratch of the bf16 batched attention: partial rows of fp16 outputs, and 16 bytes of
+// Scratch of the bf16 batched attention: partial rows of 16-bit outputs, and 16 bytes of
 // statistics each; those of the suffix items follow the context's.
 struct BatchAttnWorkspace {
     size_t part_s_off;  // the statistics; the outputs lie at 0

@@ -23,9 +23,11 @@
 //   time).  The output is divided by the sum of the rounded ones, which keeps a row that
 //   sees one key exact, the log-sum-exp uses the sum of the exact ones.
 // - Every item writes its unnormalised output and (max, sums, scale); batch_merge adds them
-//   with weights exp2(max_s - max) in a fixed order.  The outputs are written as fp16 over
-//   the row's largest element (2^-11 of an element, an eighth of what rounding O to bf16 costs,
-//   for half the traffic of float32).
+//   with weights exp2(max_s - max) in a fixed order.  The outputs are written in 16 bits, half the
+//   traffic of float32: as fp16 times a power of two that takes the row's largest element into
+//   [2^14, 2^15) (an element is off by at most 2^-11 of itself, an eighth of what rounding O to
+//   bf16 costs, down to 2^-28 of the largest, and by at most 2^-8 below, down to 2^-17 as scaled); a
+//   row with a smaller element that is not 0, as bf16 (2^-8 of each, whatever their range).
 // 64 decoding requests of 40/8 heads over 32K keys, d 128: 63 us and 7.3 of merge (its K and V once and
 // the suffixes: 37 us at 6.07 TB/s); 20 questions of 761 tokens in all, 32/8 heads, over 8K: 116 and
 // 13 (85 at 1188 TFLOP/s).  While it runs MFMA and vector unit are busy 30-42% and 39-48%, rarely
@@ -76,7 +78,7 @@ struct BaArgs {
     // Partial rows: context ones first (shared: kBaRows per segment; listed: [split][Hkv][rows of
     // the step]), suffix ones ([split][Hkv][rows of the step]) from suf_part.
     _Float16* part_o;
-    float4* part_s;          // (max, sum of rounded, sum of exact probabilities, scale)
+    float4* part_s;          // (max, sum of rounded, sum of exact probabilities, scale; -1: a row of bf16)
     size_t suf_part;
     int T, H, Hkv, G, n_sel, bshift, nb, tail;
     int ctx_wgs, suf_wgs;    // workgroups of the launch for context and suffix items
@@ -522,8 +524,8 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
             if (live) step((uint32_t)(tt % ST) * (TK * ROWB), tt * TK);
         }
 
-        // The partial rows: scaled by the largest finite element, transposed through LDS (the
-        // tiles are done with) and written as whole rows.
+        // The partial rows: in 16 bits, transposed through LDS (the tiles are done with) and
+        // written as whole rows.
         const float l_tot = ba_group_sum<NR>(l0 + l1), l_ex = ba_group_sum<NR>(e0 + e1);
         asm volatile("" : "+v"(lane));
         __syncthreads();
@@ -531,28 +533,43 @@ __global__ __launch_bounds__(kBaWaves * 64, 3) void battn_bf16(BaArgs a) {
         static_assert(kBaRows * OROW <= (int)sizeof(tiles), "the rows fit the tiles");
         char* orow = (char*)tiles + (w * NR) * OROW;
         if (live) {
+            // The largest finite element, and the smallest that is not 0 (its bits without the sign,
+            // less one: 0 is then above every number).
             float top = 0.f;
+            uint32_t low = ~0u;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int v = 0; v < NV; ++v) {
                     const float x = fabsf(o[db][v]);
                     top = x <= 3.4028235e38f ? fmaxf(top, x) : top;
+                    low = min(low, (__float_as_uint(o[db][v]) << 1) - 1u);
                 }
             top = ba_group_max<NR>(top);
-            const float inv = top > 0.f ? 1.0f / top : 1.f;
-            typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+            // Exponent of the largest (of 2^-112 at least, so that scale and inverse are normal
+            // numbers; what fp16 then cuts off is below float32's smallest).
+            const int ex = top > 0.f ? max((int)(__float_as_uint(top) >> 23), 15) : 141;
+            const float inv = __uint_as_float((uint32_t)(268 - ex) << 23);
+            const bool far = ba_group_max<NR>(ex > 31 && low < ((uint32_t)(ex - 31) << 24) - 1u ? 1.f : 0.f) > 0.f;
+            const float scale = far ? -1.f : __uint_as_float((uint32_t)(ex - 14) << 23);
+            typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+            auto half = [&](float x) { return __builtin_bit_cast(uint16_t, (_Float16)(x * inv)); };
+            auto write = [&](auto bits) {
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
+                for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int j = 0; j < NV / 4; ++j)
-                    *(f16x4*)(orow + (lane & (NR - 1)) * OROW + 2 * (db * NR + 8 * j + 4 * (lane / NR))) =
-                        f16x4{(_Float16)(o[db][4 * j] * inv), (_Float16)(o[db][4 * j + 1] * inv),
-                              (_Float16)(o[db][4 * j + 2] * inv), (_Float16)(o[db][4 * j + 3] * inv)};
+                    for (int j = 0; j < NV / 4; ++j)
+                        *(u16x4*)(orow + (lane & (NR - 1)) * OROW + 2 * (db * NR + 8 * j + 4 * (lane / NR))) =
+                            u16x4{bits(o[db][4 * j]), bits(o[db][4 * j + 1]), bits(o[db][4 * j + 2]),
+                                  bits(o[db][4 * j + 3])};
+            };
+            if (__any(far))
+                write([&](float x) { return far ? __builtin_bit_cast(uint16_t, (__bf16)x) : half(x); });
+            else
+                write(half);
             // (a NaN sum under a maximum of -inf, where no logit is a number, must not pass for a
             // split without keys)
-            if (lane < n_val)
-                a.part_s[part + lane] = float4{is_nan(l_ex) ? 0.f : m_run, l_tot, l_ex, top > 0.f ? top : 1.f};
+            if (lane < n_val) a.part_s[part + lane] = float4{is_nan(l_ex) ? 0.f : m_run, l_tot, l_ex, scale};
             __builtin_amdgcn_wave_barrier();
             _Float16* dst = a.part_o + part * D + lane * 8;
 #pragma unroll
@@ -628,7 +645,7 @@ __device__ __forceinline__ void merge_row(const BaArgs& a, const BatchSplit& sp,
         const float e = st.x == -INFINITY ? 0.f : fast_exp2(st.x - M);
         z = fmaf(e, st.y, z);
         ze = fmaf(e, st.z, ze);
-        const float wt = e * st.w;                       // (0 past the last partial)
+        const float wt = e * st.w;                       // (0 past the last partial, below 0: bf16)
         for (int j0 = 0; j0 < LN && __any(c0 + j0 < n); j0 += NG * U) {
             f16x8 v[U];
             float wj[U];
@@ -638,6 +655,21 @@ __device__ __forceinline__ void merge_row(const BaArgs& a, const BatchSplit& sp,
                 wj[u] = __shfl(wt, base + (j & (LN - 1)), 64);
                 v[u] = c0 + j0 == 0 ? v0[u]
                                     : *(const f16x8*)(a.part_o + at(min(c0 + j, n - 1)) * D + col * 8);
+            }
+            bool far = false;
+#pragma unroll
+            for (int u = 0; u < U; ++u) far |= wj[u] < 0.f;
+            if (__any(far)) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const bf16x8 b = __builtin_bit_cast(bf16x8, v[u]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float x = wj[u] < 0.f ? (float)b[i] : (float)v[u][i];
+                        acc[i] = wj[u] != 0.f ? fmaf(fabsf(wj[u]), x, acc[i]) : acc[i];
+                    }
+                }
+                continue;
             }
 #pragma unroll
             for (int u = 0; u < U; ++u)

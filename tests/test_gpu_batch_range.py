@@ -1,10 +1,11 @@
-"""Batched serving calls at the ends of their range: steps whose splits fill their launches,
-against the float64 oracle."""
+"""Batched serving calls at the ends of their range: steps whose splits fill their launches, values
+of any size next to one another; against the float64 oracle."""
 
+import numpy as np
 import pytest
 import torch
 
-from batch_harness import Step
+from batch_harness import HALF, Step, attn_tol, f64
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -24,3 +25,68 @@ def test_every_split_of_a_step_is_run(gpu_lib, T, H, H_kv, d, past, new):
     ws.view(torch.float32).fill_(float("nan"))
     s.shared(ws)
     s.check(s.reference())
+
+
+def _run(s, block):
+    lists = None
+    if block:
+        nb = -(-s.T // block)
+        lists = torch.arange(nb, dtype=torch.int32, device="cuda").expand(s.q.shape[0], s.H_kv, nb).contiguous()
+        s.blocks(block, lists)
+    else:
+        s.shared()
+    return s.reference(lists, block)
+
+
+@pytest.mark.parametrize("block", [0, 64])
+@pytest.mark.parametrize("kw", [
+    dict(past=[0, 5, 200], new=[1, 1, 1], T=700),
+    dict(past=[30], new=[1], T=9000, d=64),
+    dict(past=[3, 40], new=[40, 1], T=300, H=12, H_kv=2),
+    dict(past=[2] * 6, new=[9] * 6, T=2000, H=16, H_kv=4, d=64),
+], ids=["decode", "splits", "wide", "chunks"])
+@pytest.mark.parametrize("exps", [(0, -20), (0, -18, -26), (0, -30), (20, 0, -60), (60, -60)])
+def test_channels_of_any_size(gpu_lib, exps, kw, block):
+    """Value channels scaled by powers of two next to one another: a channel's output is that of
+    the unscaled channel times its power, so its bound is too.  Elements more than 2^28 below a
+    row's largest may be rounded to bf16 once more in each partial row: 2^-8 of each, with weights
+    that sum to one at most 2^-8 sum_j p_j |V_j| <= 2^-8 (spread + |O|)."""
+    s = Step(seed=31, **kw)
+    c = 2.0 ** torch.tensor(exps, dtype=torch.float64)[torch.arange(s.d) % len(exps)]
+    for t in (s.vc, s.vs):
+        t.copy_((t.double() * c.cuda()).to(t.dtype))
+    O, lse, spread = _run(s, block)
+    c = c.numpy()
+    tol = attn_tol(O / c, spread / c)
+    if max(exps) - min(exps) > 20:
+        tol = tol + 1.01 * HALF[BF] * (spread + np.abs(O)) / c
+    assert np.abs(f64(s.lse)[:s.n] - lse).max() <= 5e-4
+    bad = np.abs(f64(s.out)[:s.n] / c - O / c) / tol
+    assert bad.max() <= 1.0, (bad.max(), np.unravel_index(bad.argmax(), bad.shape))
+
+
+@pytest.mark.parametrize("block", [0, 16])
+@pytest.mark.parametrize("exp", [-110, -118, -127, -130])
+def test_values_near_the_types_smallest(gpu_lib, exp, block):
+    """Values down to bf16's subnormal ones: within the bound of their size and float32's smallest
+    normal number, never infinite."""
+    s = Step(past=[0, 2], new=[1, 1], T=3, seed=32)
+    for t in (s.vc, s.vs):
+        t.copy_((t.double() * 2.0 ** exp).to(t.dtype))
+    O, lse, spread = _run(s, block)
+    c = 2.0 ** exp
+    err = np.abs(f64(s.out)[:s.n] - O)
+    assert np.all(err <= attn_tol(O / c, spread / c) * c + 2.0 ** -126)
+
+
+def test_largest_values(gpu_lib):
+    """Values near bf16's largest, few enough that their unnormalised sum is a float32 number, next
+    to ordinary and tiny ones."""
+    s = Step(past=[0], new=[1], T=2, seed=33)
+    c = 2.0 ** torch.tensor([120.0, 0.0, -100.0], dtype=torch.float64)[torch.arange(s.d) % 3]
+    for t in (s.vc, s.vs):
+        t.copy_((t.double() * c.cuda()).to(t.dtype))
+    O, lse, spread = _run(s, 0)
+    c = c.numpy()
+    tol = attn_tol(O / c, spread / c) + 1.01 * HALF[BF] * (spread + np.abs(O)) / c
+    assert np.all(np.abs(f64(s.out)[:s.n] - O) / c <= tol)
