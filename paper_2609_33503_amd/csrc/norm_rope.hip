@@ -213,7 +213,10 @@ void launch(const RopeArgs& a, hipStream_t st) {
     // with four).
     const int heads = (a.q ? a.H : 0) + (a.k ? a.Hkv : 0) + (a.v ? a.Hkv : 0);
     constexpr int GROUPS = kRopeThreads / (D / 16);
-    const int rows = a.n > 1024 ? std::min(kRopeRows, (GROUPS + heads - 1) / heads) : 1;
+    int rows = a.n > 1024 ? std::min(kRopeRows, (GROUPS + heads - 1) / heads) : 1;
+    // A launch dimension holds fewer than 2^32 threads.
+    static_assert(RELAXKV_MAX_FRESH_ROWS / kRopeRows * (int64_t)kRopeThreads < (int64_t)1 << 32, "every call fits");
+    while ((int64_t)((a.n + rows - 1) / rows) * kRopeThreads >= (int64_t)1 << 32) ++rows;
     hipLaunchKernelGGL((norm_rope<T, D>), dim3((a.n + rows - 1) / rows), dim3(kRopeThreads), 0, st,
                        a, rows);
 }

@@ -4,6 +4,8 @@
 //
 //   batch_launches steps N   N random steps: every workgroup and partial row that the split of the
 //                            step's plan needs is launched and has room in the workspace.
+//   batch_launches fresh     fresh_rows up to the header's largest number of rows: the grid is one that
+//                            the hardware takes (fewer than 2^32 threads in a dimension).
 //
 // Prints "ok <checks>" and exits 0 when every check holds.
 
@@ -170,6 +172,35 @@ void steps(long n) {
     }
 }
 
+void fits(const char* name, relaxkv_status st, size_t at_least) {
+    char what[200];
+    snprintf(what, sizeof what, "%s: status %d, %zu launches", name, st, launches.size());
+    expect(st == RELAXKV_OK && launches.size() >= at_least, what);
+    for (const Launch& l : launches) {
+        const uint64_t x = (uint64_t)l.grid.x * l.block.x;
+        snprintf(what, sizeof what, "%s: grid %u x %u x %u of %u threads", name, l.grid.x, l.grid.y, l.grid.z,
+                 l.block.x);
+        expect(x > 0 && x < 1ull << 32 && l.grid.y <= 65535 && l.grid.z <= 65535 && l.block.x <= 1024, what);
+    }
+    launches.clear();
+}
+
+void fresh() {
+    char name[200];
+    for (int dtype = 0; dtype < 2; ++dtype)
+        for (int d = 64; d <= 128; d += 64)
+            for (int H : {1, 16, 31, 32, 48, 64, 1024})
+                for (int n : {1, 1024, 1025, (1 << 23), (1 << 24) - 1, 1 << 24, (1 << 24) + 1, (1 << 25) - 1,
+                              RELAXKV_MAX_FRESH_ROWS}) {
+                    const relaxkv_problem p = make(64, H, dtype && H == 1024 ? 64 : H, d, dtype);
+                    const relaxkv_rope r = {(const float*)at(0x100), nullptr, nullptr, 0.f, 16, 0};
+                    const relaxkv_rows in = {at(0x1000), nullptr, nullptr, 0, 0, 0, n};
+                    snprintf(name, sizeof name, "fresh_rows of %d rows, %d heads, d %d", n, H, d);
+                    fits(name, relaxkv_fresh_rows(&p, &r, &in, (const int32_t*)at(0x100), at(0x1000), nullptr,
+                                                  nullptr, nullptr), 1);
+                }
+}
+
 }  // namespace
 
 // The runtime's launch of `kernel<<<grid, block>>>` in three calls.
@@ -190,6 +221,7 @@ TAKE hipError_t hipGetLastError() { return hipSuccess; }
 
 int main(int argc, char** argv) {
     if (argc == 3 && !strcmp(argv[1], "steps")) steps(atol(argv[2]));
+    else if (argc == 2 && !strcmp(argv[1], "fresh")) fresh();
     else return 2;
     if (n_bad) {
         fprintf(stderr, "%ld of %ld checks failed\n", n_bad, n_checks);

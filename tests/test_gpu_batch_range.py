@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from batch_harness import HALF, Step, attn_tol, f64
+from paper_2609_33503_amd import relaxkv
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
@@ -90,3 +91,24 @@ def test_largest_values(gpu_lib):
     c = c.numpy()
     tol = attn_tol(O / c, spread / c) + 1.01 * HALF[BF] * (spread + np.abs(O)) / c
     assert np.all(np.abs(f64(s.out)[:s.n] - O) / c <= tol)
+
+
+def test_more_rows_than_a_row_per_workgroup_holds(gpu_lib):
+    """fresh_rows in place over more than 2^24 rows of 64 heads: rows at both ends and around 2^24
+    come out as in a call of their own, the others (zeros) as they were."""
+    n, H, d = (1 << 24) + 5, 64, 64
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("needs 150 GB of device memory")
+    req = relaxkv.Request(torch.zeros(1, 1, H, d, dtype=BF, device="cuda"), *torch.zeros(2, 1, H, 64, d, dtype=BF, device="cuda"), 0.5)
+    rope = relaxkv.Rope(torch.linspace(1, 0.01, 32, device="cuda"))
+    at = torch.tensor([0, 1, 1 << 23, (1 << 24) - 1, 1 << 24, n - 2, n - 1], device="cuda")
+    x, pos = torch.zeros(n, H, d, dtype=BF, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    x[at] = torch.randn(len(at), H, d, device="cuda", generator=torch.Generator("cuda").manual_seed(5)).to(BF)
+    pos[at] = at.int() + 3
+    few, want = x[at], torch.empty(len(at), H, d, dtype=BF, device="cuda")
+    req.fresh_rows(rope, pos[at], None, few, None, None, want, None)
+    assert not torch.equal(few, want)
+    req.fresh_rows(rope, pos, None, x, None, None, x, None)
+    assert torch.equal(x[at], want)
+    x[at] = 0
+    assert not any(bool(x[i:i + (1 << 20)].any()) for i in range(0, n, 1 << 20))

@@ -37,3 +37,7 @@ def test_every_workgroup_and_partial_row_of_a_step(driver):
     """Random steps: all workgroups of the plan's split are launched, all partial rows have room
     (about one float32 step in 300 has more splits than 256 workgroups and three per item)."""
     _run(driver, "steps", "300000")
+
+
+def test_launches_of_the_largest_fresh_rows(driver):
+    _run(driver, "fresh")
