@@ -275,14 +275,15 @@ __device__ __forceinline__ void topk_keys(TopkLds<W>& sm, const uint32_t (&key)[
     }
 }
 
-// One workgroup per (row, KV head) over scores in memory.
+// One workgroup per (row, KV head) over scores in memory.  The heads are the grid's second dimension:
+// 2^22 units of 1024 threads are more than one dimension holds.
 template <int W, int E>
 __global__ __launch_bounds__(W * 64) void block_topk_reg(const float* __restrict__ scores, int nb,
                                                          int k, const int32_t* __restrict__ counts,
                                                          int n_rows, int Hkv,
                                                          int32_t* __restrict__ out) {
     __shared__ TopkLds<W> sm;
-    const long unit = blockIdx.x;
+    const long unit = (long)blockIdx.x * Hkv + blockIdx.y;
     const int i0 = (threadIdx.x >> 6) * (E * 64) + (threadIdx.x & 63);
     const float* s = scores + unit * nb;                 // (within the workspace for every unit)
     float x[E];
@@ -367,7 +368,7 @@ __global__ __launch_bounds__(256) void block_topk_long(const float* __restrict__
                                                        int32_t* __restrict__ out) {
     __shared__ int hist[256], scratch[4];
     __shared__ int digit_sh, above_sh;
-    const long unit = blockIdx.x;
+    const long unit = (long)blockIdx.x * Hkv + blockIdx.y;
     const int tid = threadIdx.x;
     if (unit >= (long)min(counts[0], n_rows) * Hkv) return;
     const float* s = scores + unit * nb;
@@ -475,7 +476,7 @@ hipError_t launch_block_select(const relaxkv_problem& p, const relaxkv_batch& b,
         else launch_scores<float, 64>(p, b, block, means, q, scores, st);
     }
     auto go = [&](auto kernel, int waves) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3(waves * 64), 0, st, scores, nb, n_sel,
+        hipLaunchKernelGGL(kernel, dim3(b.n_rows, p.H_kv), dim3(waves * 64), 0, st, scores, nb, n_sel,
                            b.counts, b.n_rows, p.H_kv, blocks);
     };
     if (nb <= 512) go(block_topk_reg<4, 2>, 4);

@@ -6,6 +6,7 @@
 //                            step's plan needs is launched and has room in the workspace.
 //   batch_launches fresh     fresh_rows up to the header's largest number of rows: the grid is one that
 //                            the hardware takes (fewer than 2^32 threads in a dimension).
+//   batch_launches batch     the same of the batched calls at the header's most rows, heads and requests.
 //
 // Prints "ok <checks>" and exits 0 when every check holds.
 
@@ -75,6 +76,7 @@ relaxkv_batch bind(const relaxkv_problem& p, int n_seq, int n_rows, int room) {
     return b;
 }
 
+constexpr size_t kAll = (size_t)1 << 60;               // workspace bytes that hold everything
 const relaxkv_suffix kSuffix = {(void*)0x5000, (void*)0x6000, 0, 0, 0};
 
 long first_wgs() {
@@ -201,6 +203,40 @@ void fresh() {
                 }
 }
 
+void batch() {
+    char name[200];
+    for (int dtype = 0; dtype < 2; ++dtype)
+        for (int d = 64; d <= 128; d += 64)
+            for (int H : {1, 64, 128, 1024})
+                for (int Hkv : {1, H})
+                    for (int T : {1, 64, 8192, 2048 * 16 + 1, 4096 * 16, 4096 * 16 + 1}) {
+                        if (dtype && (H / Hkv > 256 || (int64_t)T * Hkv * d >= RELAXKV_MAX_BF16_LAYER_ELEMS)) continue;
+                        const relaxkv_problem p = make(T, H, Hkv, d, dtype);
+                        const int rows = std::min(RELAXKV_MAX_BATCH_ROWS, RELAXKV_MAX_BATCH_ROW_HEADS / H);
+                        const int nb = (T + 15) / 16;
+                        const relaxkv_batch b = bind(p, RELAXKV_MAX_SEQS, rows, 1000);
+                        auto run = [&](const char* call, relaxkv_status st, size_t k) {
+                            snprintf(name, sizeof name, "%s of %d rows, %d / %d heads, T %d, d %d, dtype %d", call,
+                                     rows, H, Hkv, T, d, dtype);
+                            fits(name, st, k);
+                        };
+                        const relaxkv_rope r = {(const float*)at(0x100), nullptr, nullptr, 0.f, 16, 0};
+                        const relaxkv_rows in = {at(0x1000), at(0x2000), at(0x3000), 0, 0, 0, rows};
+                        run("batch_plan", relaxkv_batch_plan(&p, &b, (int32_t*)at(0x100), (int32_t*)at(0x100), nullptr), 1);
+                        run("batch_rows", relaxkv_batch_rows(&p, &r, &b, &in, at(0x1000), &kSuffix, nullptr), 1);
+                        run("shared_attn", relaxkv_shared_attn(&p, &b, 0, at(0x2000), at(0x3000), at(0x4000), &kSuffix,
+                                                               at(0x8000), nullptr, at(1 << 20), kAll, nullptr), 2);
+                        run("block_means", relaxkv_block_means(&p, -1, at(0x2000), 16, at(0x8000), nullptr), 1);
+                        for (int n_sel : {1, std::min(nb, RELAXKV_MAX_SELECTED_BLOCKS)}) {
+                            run("block_select", relaxkv_block_select(&p, &b, 16, at(0x8000), at(0x4000), n_sel,
+                                                                     (int32_t*)at(0x9000), at(1 << 20), kAll, nullptr), 1);
+                            run("block_attn", relaxkv_block_attn(&p, &b, 0, at(0x2000), at(0x3000), 16,
+                                                                 (int32_t*)at(0x9000), n_sel, at(0x4000), &kSuffix,
+                                                                 at(0x8000), nullptr, at(1 << 20), kAll, nullptr), 2);
+                        }
+                    }
+}
+
 }  // namespace
 
 // The runtime's launch of `kernel<<<grid, block>>>` in three calls.
@@ -222,6 +258,7 @@ TAKE hipError_t hipGetLastError() { return hipSuccess; }
 int main(int argc, char** argv) {
     if (argc == 3 && !strcmp(argv[1], "steps")) steps(atol(argv[2]));
     else if (argc == 2 && !strcmp(argv[1], "fresh")) fresh();
+    else if (argc == 2 && !strcmp(argv[1], "batch")) batch();
     else return 2;
     if (n_bad) {
         fprintf(stderr, "%ld of %ld checks failed\n", n_bad, n_checks);

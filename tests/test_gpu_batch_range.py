@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from batch_harness import HALF, Step, attn_tol, f64
+from oracle import batch_oracle as bo
 from paper_2609_33503_amd import relaxkv
 
 pytestmark = pytest.mark.gpu
@@ -112,3 +113,27 @@ def test_more_rows_than_a_row_per_workgroup_holds(gpu_lib):
     assert torch.equal(x[at], want)
     x[at] = 0
     assert not any(bool(x[i:i + (1 << 20)].any()) for i in range(0, n, 1 << 20))
+
+
+def test_selection_of_the_largest_step(gpu_lib):
+    """block_select with the most rows and heads of a step, and 2049 blocks: against float64 scores of
+    some rows."""
+    n, H, d, block, sel = 65536, 64, 64, 16, 5
+    nb = 2049
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of device memory")
+    g = torch.Generator("cuda").manual_seed(7)
+    kc = torch.zeros(1, H, nb * block, d, dtype=BF, device="cuda")
+    req = relaxkv.Request(torch.zeros(1, 1, H, d, dtype=BF, device="cuda"), kc, kc, 0.5)
+    b = req.alloc_batch(n, n, 1)
+    z = torch.zeros(n, dtype=torch.int32, device="cuda")
+    req.plan_batch(b, z, z + 1)
+    q = torch.randn(n, H, d, device="cuda", generator=g).to(BF)
+    means = torch.randn(H, nb, d, device="cuda", generator=g).to(BF)
+    lists = torch.full((n, H, sel), -7, dtype=torch.int32, device="cuda")
+    ws = torch.empty(req._lib.relaxkv_block_select_workspace_bytes(req._ref, b.ref, block), dtype=torch.uint8,
+                     device="cuda")
+    req.block_select(b, block, means, q, lists, ws)
+    assert not bool((lists == -7).any())
+    at = [0, 1, 40000, n - 2, n - 1]
+    assert np.array_equal(lists[at].cpu().numpy(), bo.block_select(f64(q[at]), f64(means), sel))

@@ -41,3 +41,7 @@ def test_every_workgroup_and_partial_row_of_a_step(driver):
 
 def test_launches_of_the_largest_fresh_rows(driver):
     _run(driver, "fresh")
+
+
+def test_launches_of_the_largest_batches(driver):
+    _run(driver, "batch")
