@@ -86,7 +86,8 @@ struct BaArgs {
     float sl2;               // softmax scale * log2(e)
 };
 
-// The step's split, through the scalar cache (it was written by an earlier kernel).
+// The step's split, through the scalar cache (it was written by an earlier kernel).  A step without
+// rows may have no split at all (a zeroed buffer before its first plan): nothing is divided by it.
 __device__ __forceinline__ BatchSplit load_split(const int32_t* counts) {
     typedef const __attribute__((address_space(4))) int32_t const_word;
     struct Words { int32_t w[sizeof(BatchSplit) / 4]; } words;
@@ -709,6 +710,7 @@ __global__ __launch_bounds__(256) void batch_merge(BaArgs a, uint16_t* __restric
                                                    float* __restrict__ lse) {
     constexpr int LPR = D / 8;
     const BatchSplit sp = load_split(a.counts);
+    if (sp.rows == 0) return;
     int n_ctx, kps;
     if constexpr (LIST) list_split(a, sp.rows, n_ctx, kps);
     else n_ctx = sp.tiles / sp.quota + 1;
@@ -749,6 +751,7 @@ __global__ __launch_bounds__(f32_waves<LIST>() * 64, 4) void battn_f32(BaF32Args
     int* lst = (int*)(f32_lds + sizeof(Lds));
     const int rl = threadIdx.x % R;
     const BatchSplit sp = load_split(a.counts);
+    if (sp.rows == 0) return;
     int x = (int)(blockIdx.y * gridDim.x + blockIdx.x);
     bool ctx = false;
     int n_split, kps;
@@ -836,6 +839,7 @@ __global__ __launch_bounds__(256) void batch_merge_f32(BaF32Args a) {
     const int lane = threadIdx.x & 63, grp = lane / LPR, col = lane % LPR;
     const long th = blockIdx.x * 4l + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const BatchSplit sp = load_split(a.counts);
+    if (sp.rows == 0) return;
     int n = sp.f32_n + sp.f32_sn, kps;
     if constexpr (LIST) list_split_f32(a, sp.rows, n, kps);
     const long rows = (long)sp.rows * a.H;

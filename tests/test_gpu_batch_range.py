@@ -137,3 +137,22 @@ def test_selection_of_the_largest_step(gpu_lib):
     assert not bool((lists == -7).any())
     at = [0, 1, 40000, n - 2, n - 1]
     assert np.array_equal(lists[at].cpu().numpy(), bo.block_select(f64(q[at]), f64(means), sel))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_calls_before_the_first_plan(gpu_lib, dtype):
+    """A zeroed batch buffer is a step without rows: every call leaves its outputs as they were."""
+    s = Step(past=[5, 1], new=[2, 1], T=200, dtype=dtype)
+    s.batch = s.req.alloc_batch(2, 3, s.room)
+    k, q_rot = torch.zeros(3, 2, 128, dtype=dtype, device="cuda"), torch.full_like(s.q, 7.0)
+    ks, vs = s.ks.clone(), s.vs.clone()
+    s.req.batch_rows(relaxkv.Rope(), s.batch, s.q, k, k, q_rot, s.ks, s.vs)
+    lists = torch.full((3, 2, 4), -7, dtype=torch.int32, device="cuda")
+    means = torch.zeros(2, 4, 128, dtype=dtype, device="cuda")
+    s.req.block_select(s.batch, 64, means, s.q, lists, s.req.alloc_block_workspace(s.batch, 64, 4))
+    s.shared()
+    s.blocks(64, lists)
+    assert s.batch.counts_to_host() == [0, 0, 0, 0]
+    for t, v in ((q_rot, 7), (s.out, 7), (s.lse, 7), (lists, -7)):
+        assert bool((t == v).all())
+    assert torch.equal(ks.nan_to_num(9), s.ks.nan_to_num(9)) and torch.equal(vs.nan_to_num(9), s.vs.nan_to_num(9))
