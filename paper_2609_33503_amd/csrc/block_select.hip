@@ -297,13 +297,18 @@ __global__ __launch_bounds__(W * 64) void block_topk_reg(const float* __restrict
 }
 
 // Scores and top-k of one (row, KV head) in one workgroup: for steps of few rows, which are
-// bound by the latency of a launch and not by a CU's 64-bit products (84 rows of KV heads, 511
-// blocks, d 64: 7.3 us for 4.7 + 5.0 in two launches; 240, 1000 blocks: 7.5 for 4.4 + 5.5; 240, 500
-// blocks, d 128: 9.9 for 4.4 + 5.4; 64, 2048 blocks, d 128: 24 for 4.3 + 5.2).  Four lanes per block, each a quarter of the head dimension.
+// bound by the latency of a launch and not by a CU's 64-bit products.  Four lanes per block, each a
+// quarter of the head dimension.  Per call, replayed, one launch and two (8 units, rows times KV
+// heads, to 256):
+//   d 64    250 blocks 5.4-6.1 us, 7.3-8.1;   1000 blocks 7.4-8.4, 7.6-8.5
+//   d 128   250 blocks 5.9-6.6, 8.0-8.8;      500 blocks (in two passes) 8.2-13.7, 8.1-9.1
+// (float32 and bf16; the means of a second pass at d 128 went through scratch memory): one launch for
+// up to a block per thread at d 64 and one pass at d 128, and for one round of workgroups.
 constexpr int kFusedThreads = 1024;
-// Steps that take one launch: products per row (blocks times d), and units (rows times KV
-// heads) of one round of workgroups.
-constexpr long kFusedProducts = 65536, kFusedUnits = 256;
+constexpr long kFusedUnits = 256;
+inline int fused_blocks(const relaxkv_problem& p) {
+    return p.d == 64 ? kFusedThreads : kFusedThreads / 4;
+}
 template <typename T, int D>
 __global__ __launch_bounds__(kFusedThreads) void block_select_rows(const T* __restrict__ q,
                                                             const T* __restrict__ means, int nb, int k,
@@ -311,8 +316,7 @@ __global__ __launch_bounds__(kFusedThreads) void block_select_rows(const T* __re
                                                             int n_rows, int H, int Hkv, int G,
                                                             int32_t* __restrict__ out) {
     constexpr int NT = kFusedThreads, NC = D / 32, BLK = NT / 4;   // chunks of a lane, blocks at a time
-    constexpr int W = NT / 64;                           // (one block per thread in the top-k)
-    static_assert(kFusedProducts <= NT * 64, "a row's blocks have a thread each");
+    constexpr int W = NT / 64;                           // (one block per thread in the top-k: nb <= NT)
     __shared__ TopkLds<W> sm;
     __shared__ float score[NT];
     __shared__ __attribute__((aligned(16))) double qs[D];
@@ -337,7 +341,7 @@ __global__ __launch_bounds__(kFusedThreads) void block_select_rows(const T* __re
         qs[c] = s;
     }
     __syncthreads();
-    for (int b0 = 0; b0 < nb; b0 += BLK) {
+    for (int b0 = 0; b0 < (D == 64 ? nb : 1); b0 += BLK) {     // (d 128: nb <= BLK)
         const int b = b0 + (tid >> 2);
         double s = 0.0, s1 = 0.0;
 #pragma unroll
@@ -349,7 +353,7 @@ __global__ __launch_bounds__(kFusedThreads) void block_select_rows(const T* __re
                 s1 = fma(qs[part * 8 + i * 32 + e + 1], (double)mf[i][e + 1], s1);
             }
         }
-        if (b0 + BLK < nb) load(b + BLK);
+        if (D == 64 && b0 + BLK < nb) load(b + BLK);
         s += s1;
         s += __shfl_xor(s, 1, 64);
         s += __shfl_xor(s, 2, 64);
@@ -452,7 +456,7 @@ hipError_t launch_block_select(const relaxkv_problem& p, const relaxkv_batch& b,
                                float* scores, hipStream_t st) {
     const int nb = block_count(p, block);
     const long units = (long)b.n_rows * p.H_kv;
-    if ((long)nb * p.d <= kFusedProducts && units <= kFusedUnits) {
+    if (nb <= fused_blocks(p) && units <= kFusedUnits) {
         auto go = [&](auto kernel, auto q_t) {
             typedef decltype(q_t) T;
             hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3(kFusedThreads), 0, st, (const T*)q,

@@ -7,6 +7,7 @@
 //   batch_launches fresh     fresh_rows up to the header's largest number of rows: the grid is one that
 //                            the hardware takes (fewer than 2^32 threads in a dimension).
 //   batch_launches batch     the same of the batched calls at the header's most rows, heads and requests.
+//   batch_launches select    block_select takes one launch where that is the faster form.
 //
 // Prints "ok <checks>" and exits 0 when every check holds.
 
@@ -237,6 +238,29 @@ void batch() {
                     }
 }
 
+// block_select of `rows` rows and 8 KV heads over nb blocks takes n launches.
+void select_launches(int d, int dtype, int nb, int rows, size_t n) {
+    char what[200];
+    const relaxkv_problem p = make(nb * 16, 8, 8, d, dtype);
+    const relaxkv_batch b = bind(p, rows, rows, 8);
+    launches.clear();
+    expect(relaxkv_block_select(&p, &b, 16, at(0x8000), at(0x4000), 1, (int32_t*)at(0x9000), at(1 << 20), kAll,
+                                nullptr) == RELAXKV_OK, "status");
+    snprintf(what, sizeof what, "block_select: d %d, dtype %d, %d blocks, %d rows: %zu launches instead of %zu", d,
+             dtype, nb, rows, launches.size(), n);
+    expect(launches.size() == n, what);
+}
+
+void select() {
+    for (int rows : {1, 32, 33})
+        for (int nb : {1, 60, 256, 257, 500, 512, 1024, 1025}) {
+            select_launches(64, 0, nb, rows, rows <= 32 && nb <= 1024 ? 1 : 2);
+            select_launches(64, 1, nb, rows, rows <= 32 && nb <= 1024 ? 1 : 2);
+            select_launches(128, 0, nb, rows, rows <= 32 && nb <= 256 ? 1 : 2);
+            select_launches(128, 1, nb, rows, rows <= 32 && nb <= 256 ? 1 : 2);
+        }
+}
+
 }  // namespace
 
 // The runtime's launch of `kernel<<<grid, block>>>` in three calls.
@@ -259,6 +283,7 @@ int main(int argc, char** argv) {
     if (argc == 3 && !strcmp(argv[1], "steps")) steps(atol(argv[2]));
     else if (argc == 2 && !strcmp(argv[1], "fresh")) fresh();
     else if (argc == 2 && !strcmp(argv[1], "batch")) batch();
+    else if (argc == 2 && !strcmp(argv[1], "select")) select();
     else return 2;
     if (n_bad) {
         fprintf(stderr, "%ld of %ld checks failed\n", n_bad, n_checks);

@@ -45,3 +45,7 @@ def test_launches_of_the_largest_fresh_rows(driver):
 
 def test_launches_of_the_largest_batches(driver):
     _run(driver, "batch")
+
+
+def test_launches_of_the_selection(driver):
+    _run(driver, "select")
