@@ -622,31 +622,47 @@ __device__ __forceinline__ void merge_row(const BaArgs& a, const BatchSplit& sp,
         step = kBaRows;
     }
     const size_t suf = a.suf_part + (size_t)g * R + rho, suf_step = (size_t)a.Hkv * R;
+    const f32x4* part_s = (const f32x4*)a.part_s;
     auto at = [&](int s) { return s < n_ctx ? first + s * step : suf + (s - n_ctx) * suf_step; };
     // The first statistics and outputs are loaded beside the row's position, which says how many
     // suffix splits there are: up to all of them (what a split did not write gets weight 0).
     const int n_all = n_ctx + sp.suf_n;
-    const float4 none = {-INFINITY, 0.f, 0.f, 0.f};
-    float4 st0 = a.part_s[at(min(lane, n_all - 1))];
+    const f32x4 none = {-INFINITY, 0.f, 0.f, 0.f};
+    f32x4 st0 = part_s[at(min(lane, n_all - 1))];
     f16x8 v0[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
         v0[u] = *(const f16x8*)(a.part_o + at(min(u * NG + grp, n_all - 1)) * D + col * 8);
     const int n = n_ctx + (a.row_pos[t] - a.T) / sp.suf_kps + 1;
     st0 = lane < n ? st0 : none;
-    float M = st0.x;
-    for (int s = lane + LN; s < n; s += LN) M = fmaxf(M, a.part_s[at(s)].x);
+    float M = st0[0];
+    for (int s = lane + LN; s < n; s += LN) M = fmaxf(M, part_s[at(s)][0]);
 #pragma unroll
     for (int o = LN / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
     float acc[8], z = 0.f, ze = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
     for (int c0 = 0; __any(c0 < n); c0 += LN) {
-        const float4 st = c0 == 0 ? st0 : c0 + lane < n ? a.part_s[at(c0 + lane)] : none;
-        const float e = st.x == -INFINITY ? 0.f : fast_exp2(st.x - M);
-        z = fmaf(e, st.y, z);
-        ze = fmaf(e, st.z, ze);
-        const float wt = e * st.w;                       // (0 past the last partial, below 0: bf16)
+        f32x4 st = st0;
+        if (c0 > 0) st = c0 + lane < n ? part_s[at(c0 + lane)] : none;
+        const float e = st[0] == -INFINITY ? 0.f : fast_exp2(st[0] - M);
+        z = fmaf(e, st[1], z);
+        ze = fmaf(e, st[2], ze);
+        const float wt = e * st[3];                       // (0 past the last partial, below 0: bf16)
+        if (__any(st[3] < 0.f)) {                         // (rare: one partial at a time)
+            for (int j0 = 0; j0 < LN && __any(c0 + j0 < n); j0 += NG) {
+                const int j = j0 + grp;
+                const float wj = __shfl(wt, base + (j & (LN - 1)), 64);
+                const f16x8 v = *(const f16x8*)(a.part_o + at(min(c0 + j, n - 1)) * D + col * 8);
+                const bf16x8 b = __builtin_bit_cast(bf16x8, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {            // (weight 0: the output may not be written)
+                    const float x = wj < 0.f ? (float)b[i] : (float)v[i];
+                    acc[i] = wj != 0.f ? fmaf(fabsf(wj), x, acc[i]) : acc[i];
+                }
+            }
+            continue;
+        }
         for (int j0 = 0; j0 < LN && __any(c0 + j0 < n); j0 += NG * U) {
             f16x8 v[U];
             float wj[U];
@@ -656,21 +672,6 @@ __device__ __forceinline__ void merge_row(const BaArgs& a, const BatchSplit& sp,
                 wj[u] = __shfl(wt, base + (j & (LN - 1)), 64);
                 v[u] = c0 + j0 == 0 ? v0[u]
                                     : *(const f16x8*)(a.part_o + at(min(c0 + j, n - 1)) * D + col * 8);
-            }
-            bool far = false;
-#pragma unroll
-            for (int u = 0; u < U; ++u) far |= wj[u] < 0.f;
-            if (__any(far)) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const bf16x8 b = __builtin_bit_cast(bf16x8, v[u]);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float x = wj[u] < 0.f ? (float)b[i] : (float)v[u][i];
-                        acc[i] = wj[u] != 0.f ? fmaf(fabsf(wj[u]), x, acc[i]) : acc[i];
-                    }
-                }
-                continue;
             }
 #pragma unroll
             for (int u = 0; u < U; ++u)
