@@ -58,8 +58,9 @@
  *   must not overlap in time; relaxkv_query_attn_noalloc uses a device array
  *   of the library instead (see there).
  * - Compute calls enqueue kernels only (no allocation, memset or host
- *   synchronisation; relaxkv_counts_to_host is the one synchronising call),
- *   so a sequence of them can be captured into a HIP graph and replayed.
+ *   synchronisation; relaxkv_counts_to_host and relaxkv_batch_to_host are the
+ *   synchronising calls), so a sequence of them can be captured into a HIP graph
+ *   and replayed.
  * - The one piece of request state on the host is in relaxkv_sets: the set-building
  *   calls record in it which kind of target and context lists they built
  *   (global_targets, context_sets), so pass the struct the last of them
@@ -509,7 +510,9 @@ relaxkv_status relaxkv_counts_to_host(const relaxkv_sets* s, int32_t* host_count
  * The maps of a step, carved by relaxkv_batch_bind out of one caller-owned device buffer
  * and written by relaxkv_batch_plan.
  *   n_seq, n_rows, max_suffix  requests; rows that the caller's row buffers hold (>= 0; a
- *            step may have fewer); tokens of a request's suffix.
+ *            step may have fewer, at a cost: the calls launch for n_rows, so a batch with room for
+ *            some hundred times a step's rows takes up to several times as long for it as one of
+ *            its size); tokens of a request's suffix.
  *   row_off  [n_seq+1]  request b's rows are row_off[b] .. row_off[b+1]-1.
  *   row_seq  [n_rows]   request of each row, -1 behind the step's last row.
  *   row_pos  [n_rows]   position T_c + past_b + i of each row, -1 behind the last.
@@ -638,7 +641,9 @@ size_t relaxkv_shared_attn_workspace_bytes(const relaxkv_problem* p, const relax
  *             calls that share it must be ordered.
  * The same call gives the same bits on every run.  The last bits of a row depend on the
  * step's number of rows, row tiles and longest suffix, which choose the splits, but not on
- * the room of the batch (n_rows, max_suffix).
+ * the room of the batch (n_rows, max_suffix).  bf16: probabilities are rounded to bf16 for the
+ * product with V, and a split's outputs to 16 bits: by at most 2^-11 of an element down to 2^-28 of
+ * the row's largest, by at most 2^-8 of it below.
  */
 relaxkv_status relaxkv_shared_attn(const relaxkv_problem* p, const relaxkv_batch* b, int32_t layer,
                                    const void* k_cache, const void* v_cache, const void* q,

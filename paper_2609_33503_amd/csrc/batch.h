@@ -42,7 +42,7 @@ constexpr int kBaLongSuffix = 1024;    // tokens from which the suffix items go 
 // waves, 14.8 and a longer merge with 4; 65 rows of 8 heads over 200 listed and suffix keys: 18.3,
 // 20.5 with 8, 29.0 with 16).  A split's keys are at least one 16-key block for each wave.  Shared:
 // up to kBaF32More splits more where as many as kBaF32Items items leave places of the last round
-// idle (64 requests of 5 rows, 8 heads, over 32K: 543 us, 778 without).
+// idle (64 requests of 5 rows, 8 heads, over 32K: 526-543 us, 778 without).
 constexpr int kBaF32Waves = 8, kBaF32ListWaves = 4;
 constexpr int kBaF32Keys = 16 * kBaF32Waves, kBaF32ListKeys = 16 * kBaF32ListWaves;
 constexpr int kBaF32Wgs = 256, kBaF32ListWgs = 512, kBaF32Items = 512, kBaF32More = 3;

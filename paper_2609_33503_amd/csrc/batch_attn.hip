@@ -12,9 +12,12 @@
 //   every key below the count is one the row sees.
 // - Suffix items: 128 rows of one request, times one split of its keys, causal.
 // - How the items are split over workgroups (BatchSplit) follows from the step itself and
-//   comes with its plan, so a batch with room for many rows costs a small step nothing.
+//   comes with its plan, so that the room of a batch does not change how a step is computed.  The
+//   grids do follow the room, and a workgroup without an item takes its start and end: 64 decoding
+//   rows of 40/8 heads over 32K in a batch of 64 rows, 512, 4096, 16384: 72, 69, 82, 132 us; over
+//   2K listed keys 66, 68, 116, 297.
 // - Each item streams 32-key K and V tiles through three swizzled LDS buffers by direct
-//   loads; 48 KB of LDS and 165 registers let three workgroups share a CU, whose softmax,
+//   loads; 48 KB of LDS and 167 registers let three workgroups share a CU, whose softmax,
 //   matrix products and waits overlap.  A wave owns 32 rows (16 where that covers the item;
 //   one row per lane): S^T = K Q^T, online softmax in the exp2 domain with a lazily raised
 //   maximum, O^T += V^T P^T.
@@ -28,9 +31,9 @@
 //   [2^14, 2^15) (an element is off by at most 2^-11 of itself, an eighth of what rounding O to
 //   bf16 costs, down to 2^-28 of the largest, and by at most 2^-8 below, down to 2^-17 as scaled); a
 //   row with a smaller element that is not 0, as bf16 (2^-8 of each, whatever their range).
-// 64 decoding requests of 40/8 heads over 32K keys, d 128: 63 us and 7.3 of merge (its K and V once and
-// the suffixes: 37 us at 6.07 TB/s); 20 questions of 761 tokens in all, 32/8 heads, over 8K: 116 and
-// 13 (85 at 1188 TFLOP/s).  While it runs MFMA and vector unit are busy 30-42% and 39-48%, rarely
+// 64 decoding requests of 40/8 heads over 32K keys, d 128: 63 us and 7.0 of merge (its K and V once and
+// the suffixes: 37 us at 6.07 TB/s); 20 questions of 761 tokens in all, 32/8 heads, over 8K: 115-120
+// and 12 (85 at 1188 TFLOP/s).  While it runs MFMA and vector unit are busy 30-42% and 39-48%, rarely
 // together, LDS 23%.  384 rows per KV head take 49-53 us more for 32K more keys, and as much without
 // the fills, which alone take 33: the arithmetic at the clock that the power limit leaves.
 // A row that sees no key gets O = 0 and lse = -inf.
@@ -858,8 +861,7 @@ __global__ __launch_bounds__(256) void batch_merge_f32(BaF32Args a) {
         const float w = c0 + lane < n ? expf(a.part_l[(c0 + lane) * rows + th] - ref) : 0.f;
         z += w;
         const int m = min(64, n - c0);
-#pragma unroll 8
-        for (int j0 = 0; j0 < m; j0 += NG) {
+        for (int j0 = 0; j0 < m; j0 += NG) {             // (one load after another)
             const int j = min(j0 + grp, m - 1);
             float wj = __shfl(w, j, 64);
             wj = j0 + grp < m ? wj : 0.f;
@@ -1026,6 +1028,7 @@ hipError_t launch_batch_attn(const relaxkv_problem& p, const relaxkv_batch& b, i
     a.list_items = p.H_kv * ((G + kBaRows - 1) / kBaRows);
     a.list_tiles = (int)(((long)n_sel * block + kBaKeys - 1) / kBaKeys);
     a.sl2 = scale * kLog2e;
+    // (workgroups for a wave per row; with D/8 lanes per row most of them have none)
     const unsigned merges = (unsigned)(((long)b.n_rows * p.H + 3) / 4);
     auto go = [&](auto d_t, auto list_t) {
         constexpr int D = decltype(d_t)::value;

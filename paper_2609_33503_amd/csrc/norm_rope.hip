@@ -15,7 +15,9 @@
 // Angles: P f_i is exact in 64 bits (f_i is float32) and is reduced to an eighth of a turn
 // there, so positions of millions lose nothing; sine and cosine are their Taylor sums up to
 // a^9 and a^10, whose remainders are below 2e-9 for |a| <= pi/4.
-// 16411 rows of 40 query and 8 key/value heads, d 128, from a fused projection: 83.5 us, 5.6 TB/s.
+// 16411 rows of 40 query and 8 key/value heads, d 128, from a fused projection: 82 us, 5.7 TB/s (float32
+// 168, 5.6).  Fewer rows: the launch and its dependent loads (2.9 us for 4 rows), then the copy rate
+// (3001 float32 rows of 12 and 3 heads, d 64: 8.9 us; twice as many 15.0, 4.6 TB/s of what is added).
 
 #include <algorithm>
 
