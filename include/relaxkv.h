@@ -642,8 +642,8 @@ size_t relaxkv_shared_attn_workspace_bytes(const relaxkv_problem* p, const relax
  * The same call gives the same bits on every run.  The last bits of a row depend on the
  * step's number of rows, row tiles and longest suffix, which choose the splits, but not on
  * the room of the batch (n_rows, max_suffix).  bf16: probabilities are rounded to bf16 for the
- * product with V, and a split's outputs to 16 bits: by at most 2^-11 of an element down to 2^-28 of
- * the row's largest, by at most 2^-8 of it below.
+ * product with V, and a split's outputs to 16 bits: by at most 2^-11 of each element, or by at most
+ * 2^-8 in rows with an element that is not 0 below 2^-28 of the largest.
  */
 relaxkv_status relaxkv_shared_attn(const relaxkv_problem* p, const relaxkv_batch* b, int32_t layer,
                                    const void* k_cache, const void* v_cache, const void* q,

@@ -20,13 +20,22 @@ BF, F32 = torch.bfloat16, torch.float32
 ])
 def test_every_split_of_a_step_is_run(gpu_lib, T, H, H_kv, d, past, new):
     """float32 steps of 286 to 448 context items, in a workspace that holds NaN: a split that no
-    workgroup takes would show."""
-    s = Step(past=past, new=new, T=T, H=H, H_kv=H_kv, d=d, dtype=F32, seed=21,
-             room=max(p + n for p, n in zip(past, new)))
-    ws = s.req.alloc_shared_workspace(s.batch)
-    ws.view(torch.float32).fill_(float("nan"))
-    s.shared(ws)
+    workgroup takes would show.  A batch with more room gives the same bits."""
+    room = max(p + n for p, n in zip(past, new))
+    s, more = (Step(past=past, new=new, T=T, H=H, H_kv=H_kv, d=d, dtype=F32, seed=21, room=room + r, extra_rows=e)
+               for r, e in ((0, 0), (300, 700)))
+    for x in (s, more):
+        ws = x.req.alloc_shared_workspace(x.batch)
+        ws.view(torch.float32).fill_(float("nan"))
+        x.shared(ws)
     s.check(s.reference())
+    assert torch.equal(s.out, more.out[:s.n]) and torch.equal(s.lse, more.lse[:s.n])
+
+
+def _needs(gb):
+    torch.cuda.empty_cache()                         # (what earlier tests' tensors still hold)
+    if torch.cuda.mem_get_info()[0] < gb << 30:
+        pytest.skip(f"needs {gb} GB of device memory")
 
 
 def _run(s, block):
@@ -98,8 +107,7 @@ def test_more_rows_than_a_row_per_workgroup_holds(gpu_lib):
     """fresh_rows in place over more than 2^24 rows of 64 heads: rows at both ends and around 2^24
     come out as in a call of their own, the others (zeros) as they were."""
     n, H, d = (1 << 24) + 5, 64, 64
-    if torch.cuda.mem_get_info()[0] < 150 << 30:
-        pytest.skip("needs 150 GB of device memory")
+    _needs(150)
     req = relaxkv.Request(torch.zeros(1, 1, H, d, dtype=BF, device="cuda"), *torch.zeros(2, 1, H, 64, d, dtype=BF, device="cuda"), 0.5)
     rope = relaxkv.Rope(torch.linspace(1, 0.01, 32, device="cuda"))
     at = torch.tensor([0, 1, 1 << 23, (1 << 24) - 1, 1 << 24, n - 2, n - 1], device="cuda")
@@ -120,8 +128,7 @@ def test_selection_of_the_largest_step(gpu_lib):
     some rows."""
     n, H, d, block, sel = 65536, 64, 64, 16, 5
     nb = 2049
-    if torch.cuda.mem_get_info()[0] < 60 << 30:
-        pytest.skip("needs 60 GB of device memory")
+    _needs(60)
     g = torch.Generator("cuda").manual_seed(7)
     kc = torch.zeros(1, H, nb * block, d, dtype=BF, device="cuda")
     req = relaxkv.Request(torch.zeros(1, 1, H, d, dtype=BF, device="cuda"), kc, kc, 0.5)
